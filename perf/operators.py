@@ -291,7 +291,7 @@ def _quantise(blocks):
 
 
 def _finite(x):
-    top = torch.finfo(torch.bfloat16).max
+    top = 1.75 * 2.0 ** 127                                       # the largest number of a page
     return torch.where(torch.isnan(x), 0.0, x).clamp(-top, top)
 
 
@@ -454,7 +454,7 @@ def run(state):
 def _held(rows):
     """What a sequence's rows [length, hkv, d] are held as, in 64 bits."""
     x = rows.double()
-    x = torch.nan_to_num(x, nan=0.0, posinf=3.3895313892515355e38, neginf=-3.3895313892515355e38)
+    x = torch.nan_to_num(x, nan=0.0).clamp(-448.0 * 2.0 ** 119, 448.0 * 2.0 ** 119)
     full = x.shape[0] // PAGE * PAGE
     blocks = x[:full].view(-1, PAGE, x.shape[1], x.shape[2])
     largest = blocks.abs().amax(dim=(1, 3), keepdim=True)
