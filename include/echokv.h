@@ -405,6 +405,160 @@ int echokv_prefill_attn_ex(const echokv_shape *shape, const echokv_layer_cache *
                            float *lse_out, void *workspace, size_t workspace_bytes,
                            void *hip_stream);
 
+/* ---- Paged 8-bit cache --------------------------------------------------------
+ * For layers that keep their full rows (a layer outside the groups, a target
+ * before it is compressed, sequences that are parked): keys and values in 8 bits,
+ * in pages, with lengths and tables on the device.  Not in the paper; an option
+ * next to its compression.
+ *
+ * A page holds ECHOKV_PAGE_TOKENS tokens of one sequence, for every layer and KV
+ * head: page p of a layer is [n_kv_heads, 128 * d] bytes of keys and the same of
+ * values, and one scale byte per head and side (a power of two, its exponent + 127).
+ * What is stored, for rows x of a full block of 128 tokens and one KV head:
+ *   f(x)  = x, but 0 for NaN and +-448 * 2^119 for what lies beyond (infinities too): the
+ *           largest numbers a page can hold
+ *   e     = least integer >= -100 with max |f(x)| <= 448 * 2^e over the block and head
+ *   held  = 2^e * e4m3(f(x) / 2^e), rounded to nearest, ties to even
+ * The order of the bytes inside a page is the library's own (echokv_page_read
+ * reads them back).  Tokens behind a sequence's last full block are held as f(x)
+ * in bf16, in its tail, until their block is complete; so what is held depends on
+ * the rows alone and not on how many arrived at a time.  Rows are attended as they
+ * were given: keys of a model with rotary embedding come in rotated.
+ *
+ * bf16 rows and queries (shape->dtype), head_dim 64 or 128, flags == 0, otherwise
+ * ECHOKV_ERR_UNSUPPORTED; n_retained is not used.  Pointers to rows, pages, tails,
+ * queries, outputs, plans and workspaces are 16-byte aligned (ECHOKV_ERR_SHAPE, for
+ * the last two ECHOKV_ERR_WORKSPACE).  Everything that depends on lengths is read
+ * on the device: all calls can be captured in a graph, and a replayed step follows
+ * its sequences as they grow.
+ *
+ * One step of a batch:  echokv_pages_grow once, with the numbers of new tokens;
+ * then per layer echokv_page_append and echokv_page_decode_attn or
+ * echokv_page_prefill_attn, all with the plan that grow left. */
+#define ECHOKV_PAGE_TOKENS 128
+
+/* Block tables of a batch over a pool of pages, shared by the layers.  The caller
+ * starts with seq_len = 0, table = -1, free_list = the pool's page numbers in any
+ * order and *n_free = n_pages; from then on grow and release keep them. */
+typedef struct {
+  int32_t batch;      /* 1 .. 4096 */
+  int32_t max_pages;  /* full pages a sequence may hold, < 2^24; it may hold 127 tokens more */
+  int32_t n_pages;    /* pages of the pool, < 2^24 */
+  int32_t *table;     /* device [batch, max_pages] */
+  int32_t *seq_len;   /* device [batch] */
+  int32_t *free_list; /* device [n_pages], the first *n_free entries are free pages, taken from the end */
+  int32_t *n_free;    /* device [1] */
+} echokv_page_table;
+
+/* One layer's pages and tails. */
+typedef struct {
+  void *k, *v;             /* device [n_pages, n_kv_heads, 128 * d] bytes */
+  uint8_t *k_exp, *v_exp;  /* device [n_pages, n_kv_heads] */
+  void *k_tail, *v_tail;   /* device [batch, 128, D] bf16; rows past seq_len % 128 may hold anything */
+} echokv_page_cache;
+
+/* What grow leaves for the other calls.  int32 word 0 of buf is the status of the
+ * step (0 or ECHOKV_PLAN_* bits), words 16 .. 16 + batch are row_start: the new
+ * rows of sequence b are rows row_start[b] .. row_start[b + 1] - 1 of k_new, v_new,
+ * of prefill's q and out, and of row_slot, row_pos.  A plan stands for the step
+ * that made it: calls with a shape of other head counts, another batch or another
+ * max_rows than the plan's do nothing. */
+typedef struct {
+  void *buf;          /* device, echokv_page_plan_bytes(batch) */
+  size_t bytes;
+  int32_t max_rows;   /* new rows of a step at most (rows of k_new etc.), <= 2^30; 0: a plan for decode alone */
+} echokv_page_plan;
+#define ECHOKV_PLAN_BAD_LENGTH 1    /* a length, n_new or *n_free is negative or past its bound */
+#define ECHOKV_PLAN_TABLE_FULL 2    /* a sequence would pass max_pages full pages */
+#define ECHOKV_PLAN_NO_PAGES 4      /* not enough free pages */
+#define ECHOKV_PLAN_TOO_MANY_ROWS 8 /* more new rows than max_rows */
+#define ECHOKV_PLAN_NOT_FINITE 16   /* set by append: f changed a number (NaN, infinities, beyond 448 * 2^119) */
+
+size_t echokv_page_plan_bytes(int32_t batch);   /* 0 on a bad batch */
+
+/* Let every sequence grow by n_new[b] tokens: lengths, pages for the blocks that
+ * become full (from the end of free_list, in the order of sequences and blocks),
+ * table entries, the slot and position of every new row, and the plan.  All or
+ * nothing: with a status other than 0 no length and no page changes and the plan
+ * has no rows; attention over the sequences as they were still works.
+ *   n_new       : device [batch]
+ *   seq_len_out : device [batch]; t->seq_len itself or another array (then the
+ *                 call can be repeated from the same state)
+ *   n_free_out  : device [1], likewise
+ *   row_slot    : device [max_rows] or NULL: page * 128 + offset of a row in a full
+ *                 block, -1 - (b * 128 + offset) of one in the tail
+ *   row_pos     : device [max_rows] or NULL: the row's position in its sequence
+ * Entries behind the last row are left as they were. */
+int echokv_pages_grow(const echokv_shape *shape, const echokv_page_table *t,
+                      const int32_t *n_new, int32_t *seq_len_out, int32_t *n_free_out,
+                      int32_t *row_slot, int32_t *row_pos,
+                      const echokv_page_plan *plan, void *hip_stream);
+
+/* Slots of any cached tokens: rows row_start[b] .. row_start[b + 1] - 1 stand for
+ * positions first_pos[b] on of sequence b (both device, [batch + 1] and [batch],
+ * row_start not decreasing).  A position outside the sequence gets INT32_MIN; entries
+ * of rows outside row_start's range are left as they were. */
+int echokv_pages_slots(const echokv_page_table *t, const int32_t *row_start,
+                       const int32_t *first_pos, int32_t n_rows, int32_t *row_slot,
+                       void *hip_stream);
+
+/* End the sequences whose which[b] (device [batch]) is not 0: their pages go back to the
+ * free list in the order of sequences and blocks, their lengths become 0.  If the list
+ * would hold more pages than the pool has, nothing changes. */
+int echokv_pages_release(const echokv_page_table *t, const int32_t *which,
+                         void *hip_stream);
+
+/* Store the new rows of one layer.  k_new, v_new : device [>= rows, D] bf16. */
+int echokv_page_append(const echokv_shape *shape, const echokv_page_table *t,
+                       const echokv_page_cache *c, const echokv_page_plan *plan,
+                       const void *k_new, const void *v_new, void *hip_stream);
+
+/* The rows that are held at row_slot (device [n_rows]), in shape->out_dtype; exact in
+ * either type.  Rows of a slot that does not exist are left as they were. */
+int echokv_page_read(const echokv_shape *shape, const echokv_page_table *t,
+                     const echokv_page_cache *c, const int32_t *row_slot, int32_t n_rows,
+                     void *k_out, void *v_out, void *hip_stream);
+
+/* What may be done to the scores s_ij = scale * q_i . k_j (i, j positions) before the
+ * softmax; NULL, or zeros and NULLs, for nothing:
+ *   softcap    > 0: s <- softcap * tanh(s / softcap)
+ *   slopes     device [H_q] or NULL: then s <- s + slopes[h] * (j - i)
+ *   prefix_len device [batch] or NULL (prefill): the tokens j < prefix_len[b] are seen
+ *              by every query of the sequence, also by those in front of them; tokens
+ *              that are not cached yet are seen by none. */
+typedef struct {
+  float softcap;
+  const float *slopes;
+  const int32_t *prefix_len;
+} echokv_score_extras;
+
+/* Bytes of workspace of the two attention calls for a batch and a plan's max_rows
+ * (0: decode alone); 0 on a bad shape.  Partial results of split sequences. */
+size_t echokv_page_workspace_bytes(const echokv_shape *shape, int32_t batch,
+                                   int32_t max_rows);
+
+/* Each sequence's last token attends all its tokens:
+ *   q : device [batch, H_q, d];  out : device [batch, H_q, d] in out_dtype;
+ *   lse_out : device [batch, H_q] fp32 or NULL.
+ * An empty sequence gets zeros and -infinity.  Table entries outside the pool are
+ * skipped, their tokens seen by none. */
+int echokv_page_decode_attn(const echokv_shape *shape, const echokv_page_table *t,
+                            const echokv_page_cache *c, const echokv_page_plan *plan,
+                            const void *q, const echokv_score_extras *extras, void *out,
+                            float *lse_out, void *workspace, size_t workspace_bytes,
+                            void *hip_stream);
+
+/* The new rows' queries, after their append: row r of sequence b attends the tokens up to
+ * its own position, read as they are held (its own and its chunk's included).
+ *   q : device [>= rows, H_q, d];  out : the same in out_dtype;
+ *   lse_out : device [>= rows, H_q] fp32 or NULL; rows behind the last one are left as they were.
+ * Several sequences of different numbers of rows, none among them, in one call. */
+int echokv_page_prefill_attn(const echokv_shape *shape, const echokv_page_table *t,
+                             const echokv_page_cache *c, const echokv_page_plan *plan,
+                             const void *q, const echokv_score_extras *extras, void *out,
+                             float *lse_out, void *workspace, size_t workspace_bytes,
+                             void *hip_stream);
+
 /* Measurement aid (no paper passage: it exists so that a benchmark can report
  * the duration of the kernel that dominates echokv_decode_attn, the fused
  * predictor-product + attention kernel, separately from the whole call).

@@ -17,6 +17,7 @@ import numpy as np
 _LIB = None
 _call = None             # _hostcall.call or call_by_ctypes, and the addresses it is given, set by load()
 _APPEND = _WINDOW_APPEND = _DECODE = _DECODE_EX = 0
+_PAGE = {}               # the paged cache's entry points: name -> address
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libechokv.so")
 
 OK, ERR_NULL, ERR_SHAPE, ERR_DTYPE, ERR_CAPACITY, ERR_WORKSPACE, ERR_UNSUPPORTED, ERR_HIP, ERR_STATIC_LIMIT = range(9)
@@ -36,8 +37,13 @@ EXPORTS = ("echokv_status_string", "echokv_cache_append", "echokv_reconstruct",
            "echokv_mlp_workspace_bytes", "echokv_decode_attn_mlp", "echokv_profile_stream_read",
            "echokv_fit_workspace_bytes", "echokv_fit_linear", "echokv_prefill_attn_ex",
            "echokv_decode_attn_static", "echokv_profile_read_channel", "echokv_decode_path",
-           "echokv_augmented_weight_elems", "echokv_augment_weights")
+           "echokv_augmented_weight_elems", "echokv_augment_weights",
+           "echokv_page_plan_bytes", "echokv_pages_grow", "echokv_pages_slots", "echokv_pages_release",
+           "echokv_page_append", "echokv_page_read", "echokv_page_workspace_bytes", "echokv_page_decode_attn",
+           "echokv_page_prefill_attn")
 ACT_RELU, ACT_SILU = 1, 2
+PAGE_TOKENS = 128
+PLAN_BAD_LENGTH, PLAN_TABLE_FULL, PLAN_NO_PAGES, PLAN_TOO_MANY_ROWS, PLAN_NOT_FINITE = 1, 2, 4, 8, 16
 PATH_FUSED, PATH_FUSED_DIRECT, PATH_UNFUSED, PATH_ABSORBED, PATH_ABSORB_V, PATH_RETAINED_ONLY = range(6)
 
 
@@ -63,6 +69,24 @@ class DecodeExtras(C.Structure):
     _fields_ = [("rope_cos", C.c_void_p), ("rope_sin", C.c_void_p), ("rope_positions", C.c_int32),
                 ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("win_k", C.c_void_p),
                 ("win_v", C.c_void_p)]
+
+
+class PageTableC(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("table", C.c_void_p),
+                ("seq_len", C.c_void_p), ("free_list", C.c_void_p), ("n_free", C.c_void_p)]
+
+
+class PageCacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("k_tail", C.c_void_p), ("v_tail", C.c_void_p)]
+
+
+class PagePlanC(C.Structure):
+    _fields_ = [("buf", C.c_void_p), ("bytes", C.c_size_t), ("max_rows", C.c_int32)]
+
+
+class ScoreExtras(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("slopes", C.c_void_p), ("prefix_len", C.c_void_p)]
 
 
 def call_by_ctypes(address: int, *args) -> int:
@@ -174,6 +198,10 @@ def load() -> C.CDLL:
     lib.echokv_profile_read_channel.argtypes = [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
     lib.echokv_profile_stream_read.restype = C.c_int
     lib.echokv_profile_stream_read.argtypes = [C.c_void_p, C.c_size_t, C.c_int32, C.POINTER(C.c_double)]
+    lib.echokv_page_plan_bytes.restype = C.c_size_t
+    lib.echokv_page_plan_bytes.argtypes = [C.c_int32]
+    lib.echokv_page_workspace_bytes.restype = C.c_size_t
+    lib.echokv_page_workspace_bytes.argtypes = [C.POINTER(Shape), C.c_int32, C.c_int32]
     try:
         from ._hostcall import call
     except ImportError:                    # not built for this Python: the same calls, 3.5 us slower each
@@ -181,6 +209,8 @@ def load() -> C.CDLL:
     address = lambda f: C.cast(f, C.c_void_p).value
     _APPEND, _WINDOW_APPEND = address(lib.echokv_cache_append), address(lib.echokv_window_append)
     _DECODE, _DECODE_EX = address(lib.echokv_decode_attn), address(lib.echokv_decode_attn_ex)
+    _PAGE.update((n, address(getattr(lib, "echokv_" + n))) for n in (
+        "pages_grow", "pages_slots", "pages_release", "page_append", "page_read", "page_decode_attn", "page_prefill_attn"))
     _call = call
     _LIB = lib
     return lib
@@ -421,6 +451,186 @@ def augmented_weight_elems(shape: Shape) -> int:
 def augment_weights(shape: Shape, w_k, w_v, w_k_aug, w_v_aug, stream=None):
     _check(load().echokv_augment_weights(C.byref(shape), _ptr(w_k), _ptr(w_v), _ptr(w_k_aug), _ptr(w_v_aug),
                                          _stream(stream)), "echokv_augment_weights")
+
+
+# ---- paged 8-bit cache
+def _rows(t, dtype: str, least: int, what: str):
+    """Address of a tensor argument: contiguous, of the named torch dtype, at least so many elements.  An address passes as it is."""
+    if t is None or isinstance(t, int):
+        return t
+    if not hasattr(t, "is_contiguous"):
+        return _ptr(t)
+    if str(t.dtype) != "torch." + dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: not contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: not on a GPU")
+    if t.numel() < least:
+        raise ValueError(f"{what}: {t.numel()} elements where {least} are needed")
+    return t.data_ptr()
+
+
+class PageTable:
+    """Block tables of a batch over a pool of pages: int32 tensors table [batch, max_pages], seq_len [batch], free_list [n_pages], n_free [1]."""
+
+    def __init__(self, table, seq_len, free_list, n_free):
+        self.table, self.seq_len, self.free_list, self.n_free = table, seq_len, free_list, n_free
+
+    @classmethod
+    def empty(cls, batch: int, max_pages: int, n_pages: int, device="cuda") -> "PageTable":
+        """Every sequence empty, every page free (page 0 is taken first)."""
+        import torch
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32),
+                   torch.arange(n_pages - 1, -1, -1, **i32), torch.full((1,), n_pages, **i32))
+
+    @property
+    def batch(self) -> int:
+        return int(self.table.shape[0])
+
+    @property
+    def n_pages(self) -> int:
+        return int(self.free_list.shape[0])
+
+    def as_c(self) -> PageTableC:
+        batch, max_pages = self.table.shape
+        return PageTableC(batch, max_pages, self.n_pages, _rows(self.table, "int32", 0, "table"),
+                          _rows(self.seq_len, "int32", batch, "seq_len"), _rows(self.free_list, "int32", 0, "free_list"),
+                          _rows(self.n_free, "int32", 1, "n_free"))
+
+
+class PageCache:
+    """One layer's pages k, v (uint8 [n_pages, n_kv_heads, 128 * d]), scale bytes k_exp, v_exp (uint8 [n_pages, n_kv_heads]) and bf16 tails
+    k_tail, v_tail [batch, 128, n_kv_heads * d]."""
+
+    def __init__(self, k, v, k_exp, v_exp, k_tail, v_tail):
+        self.k, self.v, self.k_exp, self.v_exp, self.k_tail, self.v_tail = k, v, k_exp, v_exp, k_tail, v_tail
+
+    @classmethod
+    def empty(cls, shape: Shape, batch: int, n_pages: int, device="cuda") -> "PageCache":
+        import torch
+        h, d = shape.n_kv_heads, shape.head_dim
+        new = lambda dtype, *size: torch.empty(size, dtype=dtype, device=device)
+        return cls(*[new(torch.uint8, n_pages, h, PAGE_TOKENS * d) for _ in range(2)], *[new(torch.uint8, n_pages, h) for _ in range(2)],
+                   *[new(torch.bfloat16, batch, PAGE_TOKENS, h * d) for _ in range(2)])
+
+    def as_c(self, shape: Shape, t: PageTable) -> PageCacheC:
+        heads = t.n_pages * shape.n_kv_heads
+        page, tail = heads * PAGE_TOKENS * shape.head_dim, t.batch * PAGE_TOKENS * shape.n_kv_heads * shape.head_dim
+        return PageCacheC(_rows(self.k, "uint8", page, "k"), _rows(self.v, "uint8", page, "v"), _rows(self.k_exp, "uint8", heads, "k_exp"),
+                          _rows(self.v_exp, "uint8", heads, "v_exp"), _rows(self.k_tail, "bfloat16", tail, "k_tail"),
+                          _rows(self.v_tail, "bfloat16", tail, "v_tail"))
+
+
+class PagePlan:
+    """A step's plan: buf, a uint8 tensor of page_plan_bytes(batch) bytes, for up to max_rows new rows."""
+
+    def __init__(self, buf, batch: int, max_rows: int):
+        self.buf, self.batch, self.max_rows = buf, int(batch), int(max_rows)
+
+    @classmethod
+    def empty(cls, batch: int, max_rows: int, device="cuda") -> "PagePlan":
+        import torch
+        return cls(torch.empty(page_plan_bytes(batch), dtype=torch.uint8, device=device), batch, max_rows)
+
+    def _words(self):
+        import torch
+        return self.buf.view(torch.int32)
+
+    def status(self) -> int:
+        """PLAN_* bits of the step, 0 if all went well.  Waits for the GPU."""
+        return int(self._words()[0])
+
+    @property
+    def row_start(self):
+        """int32 [batch + 1] on the GPU: sequence b's new rows are row_start[b] .. row_start[b + 1] - 1."""
+        return self._words()[16:17 + self.batch]
+
+    def as_c(self) -> PagePlanC:
+        return PagePlanC(_rows(self.buf, "uint8", 0, "plan"), self.buf.numel() if hasattr(self.buf, "numel") else page_plan_bytes(self.batch),
+                         self.max_rows)
+
+
+def page_plan_bytes(batch: int) -> int:
+    return int(load().echokv_page_plan_bytes(int(batch)))
+
+
+def page_workspace_bytes(shape: Shape, batch: int, max_rows: int = 0) -> int:
+    return int(load().echokv_page_workspace_bytes(C.byref(_shape(shape)), int(batch), int(max_rows)))
+
+
+def pages_grow(shape: Shape, table: PageTable, n_new, plan: PagePlan, seq_len_out=None, n_free_out=None, row_slot=None, row_pos=None,
+               stream=None):
+    """seq_len_out, n_free_out: the table's own arrays unless given."""
+    load()
+    b = table.batch
+    _check(_call(_PAGE["pages_grow"], _shape(shape), table.as_c(), _rows(n_new, "int32", b, "n_new"),
+                 _rows(table.seq_len if seq_len_out is None else seq_len_out, "int32", b, "seq_len_out"),
+                 _rows(table.n_free if n_free_out is None else n_free_out, "int32", 1, "n_free_out"),
+                 _rows(row_slot, "int32", plan.max_rows, "row_slot"), _rows(row_pos, "int32", plan.max_rows, "row_pos"), plan.as_c(),
+                 _stream(stream)), "echokv_pages_grow")
+
+
+def pages_slots(table: PageTable, row_start, first_pos, row_slot, n_rows: Optional[int] = None, stream=None):
+    load()
+    n = int(row_slot.shape[0] if n_rows is None else n_rows)
+    _check(_call(_PAGE["pages_slots"], table.as_c(), _rows(row_start, "int32", table.batch + 1, "row_start"),
+                 _rows(first_pos, "int32", table.batch, "first_pos"), n, _rows(row_slot, "int32", n, "row_slot"), _stream(stream)),
+           "echokv_pages_slots")
+
+
+def pages_release(table: PageTable, which, stream=None):
+    load()
+    _check(_call(_PAGE["pages_release"], table.as_c(), _rows(which, "int32", table.batch, "which"), _stream(stream)), "echokv_pages_release")
+
+
+def page_append(shape: Shape, table: PageTable, cache: PageCache, plan: PagePlan, k_new, v_new, stream=None):
+    """k_new, v_new: bf16 [max_rows, n_kv_heads * d]; those behind the step's rows are not read."""
+    load()
+    least = plan.max_rows * shape.n_kv_heads * shape.head_dim
+    _check(_call(_PAGE["page_append"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(), _rows(k_new, "bfloat16", least, "k_new"),
+                 _rows(v_new, "bfloat16", least, "v_new"), _stream(stream)), "echokv_page_append")
+
+
+_OUT = {BF16: "bfloat16", F32: "float32"}
+
+
+def page_read(shape: Shape, table: PageTable, cache: PageCache, row_slot, k_out, v_out, n_rows: Optional[int] = None, stream=None):
+    load()
+    n = int(row_slot.shape[0] if n_rows is None else n_rows)
+    least, dtype = n * shape.n_kv_heads * shape.head_dim, _OUT.get(shape.out_dtype, "")
+    _check(_call(_PAGE["page_read"], _shape(shape), table.as_c(), cache.as_c(shape, table), _rows(row_slot, "int32", n, "row_slot"), n,
+                 _rows(k_out, dtype, least, "k_out"), _rows(v_out, dtype, least, "v_out"), _stream(stream)), "echokv_page_read")
+
+
+def _score_extras(shape: Shape, table: PageTable, softcap, slopes, prefix_len) -> Optional[ScoreExtras]:
+    if not softcap and slopes is None and prefix_len is None:
+        return None
+    return ScoreExtras(float(softcap), _rows(slopes, "float32", shape.n_q_heads, "slopes"), _rows(prefix_len, "int32", table.batch, "prefix_len"))
+
+
+def page_decode_attn(shape: Shape, table: PageTable, cache: PageCache, plan: PagePlan, q, out, lse_out, workspace, softcap: float = 0.0,
+                     slopes=None, stream=None):
+    """slopes: float32 [n_q_heads] on the GPU."""
+    load()
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rows = table.batch * shape.n_q_heads
+    _check(_call(_PAGE["page_decode_attn"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(),
+                 _rows(q, "bfloat16", rows * shape.head_dim, "q"), _score_extras(shape, table, softcap, slopes, None),
+                 _rows(out, _OUT.get(shape.out_dtype, ""), rows * shape.head_dim, "out"), _rows(lse_out, "float32", rows, "lse_out"),
+                 _ptr(workspace), nbytes, _stream(stream)), "echokv_page_decode_attn")
+
+
+def page_prefill_attn(shape: Shape, table: PageTable, cache: PageCache, plan: PagePlan, q, out, lse_out, workspace, softcap: float = 0.0,
+                      slopes=None, prefix_len=None, stream=None):
+    """q, out: [max_rows, n_q_heads, d], lse_out [max_rows, n_q_heads]; slopes: float32 [n_q_heads], prefix_len: int32 [batch], both on the GPU."""
+    load()
+    rows = plan.max_rows * shape.n_q_heads
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_call(_PAGE["page_prefill_attn"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(), _rows(q, "bfloat16", rows * shape.head_dim, "q"),
+                 _score_extras(shape, table, softcap, slopes, prefix_len), _rows(out, _OUT.get(shape.out_dtype, ""), rows * shape.head_dim, "out"),
+                 _rows(lse_out, "float32", rows, "lse_out"), _ptr(workspace), nbytes, _stream(stream)), "echokv_page_prefill_attn")
 
 
 def profile_stream_read(buf, repeats: int = 5) -> float:

@@ -1,0 +1,281 @@
+// libechokv: C-ABI entry points of the paged 8-bit cache.  Host side only validates and launches; lengths, tables and the sharing out
+// of work live on the device (page_kernels.h), so that a captured step follows its sequences as they grow.
+#include "../../include/echokv.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+#include <type_traits>
+
+#include "page_attn.h"
+
+using namespace echokv;
+
+namespace {
+
+#define LAUNCH_CHECK() do { if (hipGetLastError() != hipSuccess) return ECHOKV_ERR_HIP; } while (0)
+
+struct Sizes { int H_q, H_kv, G, d, D; bool out_bf16; float scale; };
+
+int check_shape(const echokv_shape* s, Sizes* o) {
+  if (!s) return ECHOKV_ERR_NULL;
+  if (s->dtype != ECHOKV_BF16 && s->dtype != ECHOKV_F32) return ECHOKV_ERR_DTYPE;
+  if (s->out_dtype != ECHOKV_BF16 && s->out_dtype != ECHOKV_F32) return ECHOKV_ERR_DTYPE;
+  if (s->n_q_heads <= 0 || s->n_kv_heads <= 0 || s->head_dim <= 0 || s->n_q_heads % s->n_kv_heads) return ECHOKV_ERR_SHAPE;
+  if (s->n_kv_heads > 4096 || s->n_q_heads > 65536 || !std::isfinite(s->softmax_scale)) return ECHOKV_ERR_SHAPE;
+  if (s->head_dim != 64 && s->head_dim != 128) return ECHOKV_ERR_UNSUPPORTED;
+  if (s->dtype != ECHOKV_BF16 || s->flags) return ECHOKV_ERR_UNSUPPORTED;
+  *o = {s->n_q_heads, s->n_kv_heads, s->n_q_heads / s->n_kv_heads, s->head_dim, s->n_kv_heads * s->head_dim, s->out_dtype == ECHOKV_BF16,
+        s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / std::sqrt((float)s->head_dim)};
+  return ECHOKV_OK;
+}
+
+int check_table(const echokv_page_table* t) {
+  if (!t) return ECHOKV_ERR_NULL;
+  if (t->batch <= 0 || t->max_pages <= 0 || t->n_pages <= 0) return ECHOKV_ERR_SHAPE;
+  if (t->batch > page::kMaxBatch || t->max_pages >= 1 << 24 || t->n_pages >= 1 << 24) return ECHOKV_ERR_UNSUPPORTED;
+  if (!t->table || !t->seq_len || !t->free_list || !t->n_free) return ECHOKV_ERR_NULL;
+  return ECHOKV_OK;
+}
+
+bool aligned16(std::initializer_list<const void*> ps) {
+  return std::all_of(ps.begin(), ps.end(), [](const void* p) { return ((uintptr_t)p & 15) == 0; });
+}
+
+int check_cache(const echokv_page_cache* c) {
+  if (!c || !c->k || !c->v || !c->k_exp || !c->v_exp || !c->k_tail || !c->v_tail) return ECHOKV_ERR_NULL;
+  return aligned16({c->k, c->v, c->k_tail, c->v_tail}) ? ECHOKV_OK : ECHOKV_ERR_SHAPE;
+}
+
+size_t plan_bytes(int batch) { return ((page::kHeadWords + (size_t)page::Plan::kArrays * (batch + 1)) * 4 + 255) / 256 * 256; }
+
+int check_plan(const echokv_page_plan* p, int batch) {
+  if (!p || !p->buf) return ECHOKV_ERR_NULL;
+  if (p->max_rows < 0 || p->max_rows > 1 << 30) return ECHOKV_ERR_SHAPE;
+  if (p->bytes < plan_bytes(batch) || !aligned16({p->buf})) return ECHOKV_ERR_WORKSPACE;
+  return ECHOKV_OK;
+}
+
+// ---- launches: items at most, and what they are shared out to.  grow (on the device) and the attention entry points go by the same numbers.
+struct Schedule {
+  int col_tiles, dec_items, pf_items;
+  int64_t dec_grid, pf_grid, pf_parts;      // items of a launch / of a split prefill launch, at most
+};
+Schedule schedule(const Sizes& z, int batch, int max_rows) {
+  Schedule s;
+  s.col_tiles = (z.G + 15) / 16;
+  s.dec_items = std::max(1, page::kDecodeItems / (z.H_kv * s.col_tiles));
+  s.dec_grid = s.dec_items + 2 * (int64_t)batch;
+  const int64_t cols = (int64_t)max_rows * z.G, most = cols / page::kQCols + std::min(batch, max_rows);
+  const bool split = max_rows > 0 && (cols + page::kQCols - 1) / page::kQCols * z.H_kv < page::kPfFill;
+  s.pf_items = split ? std::max(1, page::kPfShares / z.H_kv) : 0;
+  s.pf_parts = split ? s.pf_items + std::min<int64_t>(most, page::kPfFill / z.H_kv + 1) : 0;
+  s.pf_grid = std::max(most, s.pf_parts);
+  return s;
+}
+
+int launch_dims(int64_t blocks, int threads, dim3* grid) {
+  if (blocks * threads >= (int64_t)1 << 32) return ECHOKV_ERR_UNSUPPORTED;
+  *grid = dim3((unsigned)blocks);
+  return ECHOKV_OK;
+}
+
+int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cache* c, const echokv_page_plan* p, const void* q,
+              const echokv_score_extras* x, void* out, float* lse, const Schedule& s, page::AttnArgs* a) {
+  if (!q || !out) return ECHOKV_ERR_NULL;
+  if (!aligned16({q, out}) || ((uintptr_t)lse & 3)) return ECHOKV_ERR_SHAPE;
+  if (x && (!std::isfinite(x->softcap) || x->softcap < 0.f)) return ECHOKV_ERR_SHAPE;
+  *a = page::AttnArgs{};
+  a->k = (const uint8_t*)c->k; a->v = (const uint8_t*)c->v; a->ke = c->k_exp; a->ve = c->v_exp;
+  a->kt = (const bf16_t*)c->k_tail; a->vt = (const bf16_t*)c->v_tail; a->q = (const bf16_t*)q;
+  a->table = t->table; a->out = out; a->lse = lse;
+  a->plan = {(int32_t*)p->buf, t->batch};
+  a->key = {t->batch, z.H_q, z.H_kv, p->max_rows};
+  a->scale = z.scale; a->max_pages = t->max_pages; a->n_pages = t->n_pages; a->G = z.G; a->col_tiles = s.col_tiles;
+  if (x) { a->cap = x->softcap; a->slopes = x->slopes; a->prefix = x->prefix_len; }
+  return ECHOKV_OK;
+}
+
+// Partials in the workspace: outputs, then (maximum, sum) pairs.
+size_t part_bytes(int64_t rows, int d) { return (size_t)rows * (d + 2) * 4; }
+
+template <class F> int by_type(const Sizes& z, const page::AttnArgs& a, F f) {
+  const bool mods = a.cap > 0.f || a.slopes;
+  auto typed = [&](auto hd, auto md) { return z.out_bf16 ? f(hd, md, bf16_t{}) : f(hd, md, float{}); };
+  auto modded = [&](auto hd) { return mods ? typed(hd, std::true_type{}) : typed(hd, std::false_type{}); };
+  return z.d == 64 ? modded(std::integral_constant<int, 64>{}) : modded(std::integral_constant<int, 128>{});
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t echokv_page_plan_bytes(int32_t batch) { return batch > 0 && batch <= page::kMaxBatch ? plan_bytes(batch) : 0; }
+
+size_t echokv_page_workspace_bytes(const echokv_shape* shape, int32_t batch, int32_t max_rows) {
+  Sizes z;
+  if (check_shape(shape, &z) || batch <= 0 || batch > page::kMaxBatch || max_rows < 0 || max_rows > 1 << 30) return 0;
+  const Schedule s = schedule(z, batch, max_rows);
+  const size_t dec = part_bytes(s.dec_grid * z.H_q, z.d), pf = part_bytes(s.pf_parts * z.H_kv * page::kQCols, z.d);
+  return (std::max(dec, pf) + 255) / 256 * 256;
+}
+
+int echokv_pages_grow(const echokv_shape* shape, const echokv_page_table* t, const int32_t* n_new, int32_t* seq_len_out, int32_t* n_free_out,
+                      int32_t* row_slot, int32_t* row_pos, const echokv_page_plan* plan, void* hip_stream) {
+  Sizes z;
+  int rc = check_shape(shape, &z);
+  if (rc) return rc;
+  if ((rc = check_table(t)) || (rc = check_plan(plan, t->batch))) return rc;
+  if (!n_new || !seq_len_out || !n_free_out) return ECHOKV_ERR_NULL;
+  const Schedule s = schedule(z, t->batch, plan->max_rows);
+  page::GrowArgs a;
+  a.len0 = t->seq_len; a.n_new = n_new; a.free_list = t->free_list; a.n_free0 = t->n_free;
+  a.len1 = seq_len_out; a.n_free1 = n_free_out; a.table = t->table; a.slot = row_slot; a.pos = row_pos;
+  a.plan = {(int32_t*)plan->buf, t->batch};
+  a.max_pages = t->max_pages; a.n_pages = t->n_pages; a.max_rows = plan->max_rows; a.H_q = z.H_q; a.H_kv = z.H_kv;
+  a.dec_items = s.dec_items; a.pf_items = s.pf_items;
+  a.rows_here = plan->max_rows <= 4096;
+  const hipStream_t st = (hipStream_t)hip_stream;
+  if (t->batch <= 256 && plan->max_rows <= 1024) hipLaunchKernelGGL(page::grow_kernel<256>, dim3(1), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(page::grow_kernel<1024>, dim3(1), dim3(1024), 0, st, a);
+  LAUNCH_CHECK();
+  if (!a.rows_here) {
+    hipLaunchKernelGGL(page::grow_rows_kernel, dim3((plan->max_rows + 255) / 256), dim3(256), 0, st, a);
+    LAUNCH_CHECK();
+  }
+  return ECHOKV_OK;
+}
+
+int echokv_pages_slots(const echokv_page_table* t, const int32_t* row_start, const int32_t* first_pos, int32_t n_rows, int32_t* row_slot,
+                       void* hip_stream) {
+  const int rc = check_table(t);
+  if (rc) return rc;
+  if (n_rows < 0) return ECHOKV_ERR_SHAPE;
+  if (n_rows == 0) return ECHOKV_OK;
+  if (!row_start || !first_pos || !row_slot) return ECHOKV_ERR_NULL;
+  const page::SlotArgs a = {t->table, t->seq_len, row_start, first_pos, row_slot, t->batch, t->max_pages, n_rows};
+  hipLaunchKernelGGL(page::slots_kernel, dim3((unsigned)(((int64_t)n_rows + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream, a);
+  LAUNCH_CHECK();
+  return ECHOKV_OK;
+}
+
+int echokv_pages_release(const echokv_page_table* t, const int32_t* which, void* hip_stream) {
+  const int rc = check_table(t);
+  if (rc) return rc;
+  if (!which) return ECHOKV_ERR_NULL;
+  const page::ReleaseArgs a = {which, t->table, t->seq_len, t->free_list, t->n_free, t->batch, t->max_pages, t->n_pages};
+  hipLaunchKernelGGL(page::release_kernel<1024>, dim3(1), dim3(1024), 0, (hipStream_t)hip_stream, a);
+  LAUNCH_CHECK();
+  return ECHOKV_OK;
+}
+
+int echokv_page_append(const echokv_shape* shape, const echokv_page_table* t, const echokv_page_cache* c, const echokv_page_plan* plan,
+                       const void* k_new, const void* v_new, void* hip_stream) {
+  Sizes z;
+  int rc = check_shape(shape, &z);
+  if (rc) return rc;
+  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, t->batch))) return rc;
+  if (plan->max_rows == 0) return ECHOKV_OK;
+  if (!k_new || !v_new) return ECHOKV_ERR_NULL;
+  if (!aligned16({k_new, v_new})) return ECHOKV_ERR_SHAPE;
+  page::StoreArgs a;
+  a.k = (uint8_t*)c->k; a.v = (uint8_t*)c->v; a.ke = c->k_exp; a.ve = c->v_exp; a.kt = (bf16_t*)c->k_tail; a.vt = (bf16_t*)c->v_tail;
+  a.kn = (const bf16_t*)k_new; a.vn = (const bf16_t*)v_new; a.table = t->table;
+  a.plan = {(int32_t*)plan->buf, t->batch};
+  a.key = {t->batch, z.H_q, z.H_kv, plan->max_rows};
+  a.max_pages = t->max_pages; a.n_pages = t->n_pages;
+  dim3 grid;
+  // a sequence has an item for every block that is completed, at least one if it has new rows at all
+  const int64_t items = plan->max_rows / page::kTokens + std::min(t->batch, plan->max_rows);
+  if ((rc = launch_dims(items * z.H_kv, 256, &grid))) return rc;
+  if (z.d == 64) hipLaunchKernelGGL(page::append_kernel<64>, grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+  else hipLaunchKernelGGL(page::append_kernel<128>, grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+  LAUNCH_CHECK();
+  return ECHOKV_OK;
+}
+
+int echokv_page_read(const echokv_shape* shape, const echokv_page_table* t, const echokv_page_cache* c, const int32_t* row_slot, int32_t n_rows,
+                     void* k_out, void* v_out, void* hip_stream) {
+  Sizes z;
+  int rc = check_shape(shape, &z);
+  if (rc) return rc;
+  if ((rc = check_table(t)) || (rc = check_cache(c))) return rc;
+  if (n_rows < 0) return ECHOKV_ERR_SHAPE;
+  if (n_rows == 0) return ECHOKV_OK;
+  if (!row_slot || !k_out || !v_out) return ECHOKV_ERR_NULL;
+  if (!aligned16({k_out, v_out})) return ECHOKV_ERR_SHAPE;
+  dim3 grid;
+  if ((rc = launch_dims(((int64_t)n_rows + page::kTokens - 1) / page::kTokens * z.H_kv, 256, &grid))) return rc;
+  auto run = [&](auto hd, auto to) {
+    using TO = decltype(to);
+    page::ReadArgs<TO> a = {(const uint8_t*)c->k, (const uint8_t*)c->v, c->k_exp, c->v_exp, (const bf16_t*)c->k_tail, (const bf16_t*)c->v_tail,
+                            row_slot, (TO*)k_out, (TO*)v_out, n_rows, t->n_pages, t->batch, z.H_kv};
+    hipLaunchKernelGGL((page::read_kernel<decltype(hd)::value, TO>), grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+  };
+  auto typed = [&](auto hd) { if (z.out_bf16) run(hd, bf16_t{}); else run(hd, float{}); };
+  if (z.d == 64) typed(std::integral_constant<int, 64>{}); else typed(std::integral_constant<int, 128>{});
+  LAUNCH_CHECK();
+  return ECHOKV_OK;
+}
+
+int echokv_page_decode_attn(const echokv_shape* shape, const echokv_page_table* t, const echokv_page_cache* c, const echokv_page_plan* plan,
+                            const void* q, const echokv_score_extras* extras, void* out, float* lse_out, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  Sizes z;
+  int rc = check_shape(shape, &z);
+  if (rc) return rc;
+  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, t->batch))) return rc;
+  const Schedule s = schedule(z, t->batch, plan->max_rows);
+  page::AttnArgs a;
+  if ((rc = attn_args(z, t, c, plan, q, extras, out, lse_out, s, &a))) return rc;
+  const int64_t rows = s.dec_grid * z.H_q;
+  if (!workspace || !aligned16({workspace}) || workspace_bytes < part_bytes(rows, z.d)) return ECHOKV_ERR_WORKSPACE;
+  a.part_o = (float*)workspace;
+  a.part_ml = a.part_o + rows * z.d;
+  dim3 grid, merge;
+  if ((rc = launch_dims(s.dec_grid * z.H_kv * s.col_tiles, 256, &grid)) || (rc = launch_dims((int64_t)t->batch * z.H_q, 256, &merge))) return rc;
+  return by_type(z, a, [&](auto hd, auto md, auto to) -> int {
+    constexpr int HD = decltype(hd)::value;
+    using TO = decltype(to);
+    hipLaunchKernelGGL((page::decode_kernel<HD, decltype(md)::value, TO>), grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+    LAUNCH_CHECK();
+    hipLaunchKernelGGL((page::decode_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a);
+    LAUNCH_CHECK();
+    return ECHOKV_OK;
+  });
+}
+
+int echokv_page_prefill_attn(const echokv_shape* shape, const echokv_page_table* t, const echokv_page_cache* c, const echokv_page_plan* plan,
+                             const void* q, const echokv_score_extras* extras, void* out, float* lse_out, void* workspace,
+                             size_t workspace_bytes, void* hip_stream) {
+  Sizes z;
+  int rc = check_shape(shape, &z);
+  if (rc) return rc;
+  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, t->batch))) return rc;
+  if (plan->max_rows == 0) return ECHOKV_OK;
+  const Schedule s = schedule(z, t->batch, plan->max_rows);
+  page::AttnArgs a;
+  if ((rc = attn_args(z, t, c, plan, q, extras, out, lse_out, s, &a))) return rc;
+  const int64_t rows = s.pf_parts * z.H_kv * page::kQCols;
+  if (rows && (!workspace || !aligned16({workspace}) || workspace_bytes < part_bytes(rows, z.d))) return ECHOKV_ERR_WORKSPACE;
+  a.part_o = (float*)workspace;
+  a.part_ml = a.part_o + rows * z.d;
+  dim3 grid, merge;
+  if ((rc = launch_dims(s.pf_grid * z.H_kv, page::kPfThreads, &grid)) || (rc = launch_dims(s.pf_parts * z.H_kv, 256, &merge))) return rc;
+  merge.y = page::kQCols / 16;
+  return by_type(z, a, [&](auto hd, auto md, auto to) -> int {
+    constexpr int HD = decltype(hd)::value;
+    using TO = decltype(to);
+    hipLaunchKernelGGL((page::prefill_kernel<HD, decltype(md)::value, TO>), grid, dim3(page::kPfThreads), 0, (hipStream_t)hip_stream, a);
+    LAUNCH_CHECK();
+    if (s.pf_parts) {
+      hipLaunchKernelGGL((page::prefill_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a);
+      LAUNCH_CHECK();
+    }
+    return ECHOKV_OK;
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,507 @@
+// The paged 8-bit cache: block tables, storing and reading back.
+//
+// A page holds 128 tokens of one sequence, for every KV head of a layer.  A (page, head) is a 128 x d matrix of keys and one of values, e4m3
+// times one power of two each.  Both are stored in the order in which the matrix pipe takes them (see k_offset, v_offset), so that
+// a wave of the attention kernels loads its operands with 16 bytes per lane, consecutive lanes at consecutive addresses, and the value
+// matrix comes transposed without a transposition.  That is possible because only whole blocks are quantised: the tokens behind a sequence's
+// last full block stay in bf16 rows (the tail) until their block is complete, which also makes the stored bytes a function
+// of the block's rows alone, however they arrived.
+#pragma once
+#include "common.h"
+
+namespace echokv {
+namespace page {
+
+constexpr int kTokens = 128;            // of a page
+constexpr int kMaxBatch = 4096;         // sequences: their prefix sums fit LDS
+constexpr int kMinExp = -100;           // least exponent of a scale: products of two of them and of a query stay normal numbers
+constexpr int kQCols = 384;             // (query, query head) columns of a prefill workgroup
+constexpr int kPfFill = 256;            // prefill workgroups that fill the chip, one to a compute unit: fewer are split over the keys
+
+// ---- plan: what grow leaves for the other kernels, int32 words.  Words 16 on: row_start, then the arrays below, each of batch + 1 words.
+enum { kStatus, kRows, kDecChunk, kDecItems, kPfChunk, kPfItems, kAppItems, kNewPages, kFree0, kBatch, kHq, kHkv, kMaxRows, kMagic, kHeadWords = 16 };
+constexpr int32_t kMagicWord = 0x45504731;
+struct Plan {
+  int32_t* w;
+  int n;                                // batch
+  __host__ __device__ int32_t* arr(int i) const { return w + kHeadWords + i * (n + 1); }
+  __host__ __device__ int32_t* row_start() const { return arr(0); }      // prefix sums of the new rows
+  __host__ __device__ int32_t* len() const { return arr(1); }            // lengths with the new tokens
+  __host__ __device__ int32_t* app() const { return arr(2); }            // prefix sums of append's items
+  __host__ __device__ int32_t* dec() const { return arr(3); }            // ... of decode's items
+  __host__ __device__ int32_t* pf() const { return arr(4); }             // ... of prefill's items
+  __host__ __device__ int32_t* fresh() const { return arr(5); }          // ... of the new pages
+  static constexpr int kArrays = 6;
+};
+
+// What the attention kernels make of a plan: sizes of the call that made it.
+struct PlanKey { int batch, H_q, H_kv, max_rows; };
+__device__ __forceinline__ bool made_for(const Plan& p, const PlanKey& k) {
+  return p.w[kMagic] == kMagicWord && p.w[kBatch] == k.batch && p.w[kHq] == k.H_q && p.w[kHkv] == k.H_kv && p.w[kMaxRows] == k.max_rows;
+}
+
+// The sequence that item x belongs to, by all lanes of a wave: how many of start[1 .. n] are at most x.
+__device__ __forceinline__ int find_item(const int32_t* start, int n, int x) {
+  const int lane = threadIdx.x & 63;
+  int at = 0;
+  for (int base = 0; base < n; base += 64) {
+    const bool below = base + lane < n && start[base + lane + 1] <= x;
+    const int c = __popcll(__ballot(below));
+    at += c;
+    if (c < 64) break;
+  }
+  return __builtin_amdgcn_readfirstlane(at);
+}
+
+// ---- page layout, byte offsets inside one head's 128 * d
+// Keys: 16-byte chunk of a lane (r = token % 16, g) of the 16-token tile t: dims 8 g .. 8 g + 7 of two 32-dim steps of the product.
+template <int HD> __device__ __forceinline__ int k_offset(int token, int dim) {
+  const int t = token >> 4, r = token & 15, h = dim >> 6, half = (dim >> 5) & 1, g = (dim >> 3) & 3;
+  return ((t * (HD / 64) + h) * 64 + g * 16 + r) * 16 + half * 8 + (dim & 7);
+}
+// Values: chunk of a lane (r = dim % 16, g) of the 16-dim tile u and the 64-token half: the tokens whose probabilities the same lane group
+// holds after the product with the keys, 4 g .. 4 g + 3 of each of four 16-token tiles.
+template <int HD> __device__ __forceinline__ int v_offset(int token, int dim) {
+  const int h = token >> 6, tile = (token >> 4) & 3, g = (token >> 2) & 3, i = token & 3, u = dim >> 4, r = dim & 15;
+  return ((h * (HD / 16) + u) * 64 + g * 16 + r) * 16 + tile * 4 + i;
+}
+
+__device__ __forceinline__ float exp_to_scale(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+
+// e4m3 pair -> bf16 pair times a power of two; exact (4 significant bits, exponents far inside bf16's).
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+template <bool HI> __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, HI));
+}
+__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b, float scale) {
+  return make_uint4(widen<false>(a, scale), widen<true>(a, scale), widen<false>(b, scale), widen<true>(b, scale));
+}
+
+// A stored value: NaN as zero, what lies past 448 * 2^119 = 1.75 * 2^127 as that (the next number of a page would be 2^128, past bf16's).
+__device__ __forceinline__ uint32_t finite_bits(uint32_t b) {        // b: 16 bits
+  const uint32_t m = b & 0x7fffu;
+  return m <= 0x7f60u ? b : m <= 0x7f80u ? (b & 0x8000u) | 0x7f60u : 0;
+}
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& odd) {
+  const uint32_t lo = w & 0xffffu, hi = w >> 16, a = finite_bits(lo), b = finite_bits(hi);
+  odd |= a != lo || b != hi;
+  return a | (b << 16);
+}
+__device__ __forceinline__ uint4 finite8(uint4 x, bool& odd) {
+  return make_uint4(finite_pair(x.x, odd), finite_pair(x.y, odd), finite_pair(x.z, odd), finite_pair(x.w, odd));
+}
+
+// ---- lengths -> tables
+struct GrowArgs {
+  const int32_t *len0, *n_new, *free_list, *n_free0;
+  int32_t *len1, *n_free1, *table, *slot, *pos;
+  Plan plan;
+  int max_pages, n_pages, max_rows, H_q, H_kv;
+  int dec_items, pf_items;              // items that share the work of a decode / prefill launch; pf_items = 0: blocks of queries suffice
+  int rows_here;                        // the rows' slots are written by this launch, too
+};
+
+// One row's slot and, where the row completes a block, the block's table entry.
+__device__ __forceinline__ void grow_row(const GrowArgs& a, int row, int b, int row0, int len1, int n, int fresh, int n_free0) {
+  const int len0 = len1 - n, p = len0 + row - row0, blk = p / kTokens, full1 = len1 / kTokens;
+  int slot = -1 - (b * kTokens + p % kTokens);
+  if (blk < full1) {                                   // a block with a new row is a new page
+    const int page = a.free_list[n_free0 - 1 - (fresh + blk - len0 / kTokens)];
+    slot = page * kTokens + p % kTokens;
+    if (p % kTokens == kTokens - 1) a.table[(int64_t)b * a.max_pages + blk] = page;
+  }
+  if (a.slot) a.slot[row] = slot;
+  if (a.pos) a.pos[row] = p;
+}
+
+// Sums over the block's threads, in every thread.
+template <int N, int NT> __device__ __forceinline__ void block_sums(int64_t (&v)[N], int64_t (*lds)[NT / 64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    for (int o = 32; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o, 64);
+    if (lane == 0) lds[i][wave] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    int64_t s = 0;
+    for (int k = 0; k < NT / 64; ++k) s += lds[i][k];
+    v[i] = s;
+  }
+  __syncthreads();
+}
+
+// All or nothing: lengths, sums and chunk sizes by one workgroup, a thread per sequence.
+template <int NT>
+__global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
+  __shared__ int64_t red[6][NT / 64];
+  __shared__ int32_t wsum[5][NT / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = a.plan.n, G = a.H_q / a.H_kv;
+  const int64_t cap = (int64_t)a.max_pages * kTokens + kTokens - 1;
+  const int n_free0 = *a.n_free0;
+  // rows, new pages, 64-token halves of full pages, query blocks, their halves; bits of what is wrong
+  int64_t s[6] = {0, 0, 0, 0, 0, 0};
+  uint32_t wrong = 0;
+  for (int b = tid; b < B; b += NT) {
+    const int64_t l = a.len0[b], n = a.n_new[b];
+    if (l < 0 || l > cap || n < 0) { wrong |= 1; continue; }
+    if (l + n > cap) { wrong |= 2; continue; }
+    const int64_t t = l + n, qb = (n * G + kQCols - 1) / kQCols;
+    s[0] += n; s[1] += t / kTokens - l / kTokens; s[2] += t / kTokens * 2; s[3] += qb; s[4] += qb * ((t + 63) / 64);
+  }
+  s[5] = (wrong & 1 ? 1 : 0) + (wrong & 2 ? (int64_t)1 << 32 : 0);
+  block_sums<6, NT>(s, red);
+  int status = 0;
+  if ((s[5] & 0xffffffff) || n_free0 < 0 || n_free0 > a.n_pages) status |= 1;      // ECHOKV_PLAN_BAD_LENGTH
+  if (s[5] >> 32) status |= 2;                                                     // ECHOKV_PLAN_TABLE_FULL
+  if (!status && s[1] > n_free0) status |= 4;                                      // ECHOKV_PLAN_NO_PAGES
+  if (!status && s[0] > a.max_rows) status |= 8;                                   // ECHOKV_PLAN_TOO_MANY_ROWS
+  const bool ok = status == 0;
+  if (!ok) {                                           // nobody grows: the halves of the lengths as they were
+    s[0] = s[1] = s[2] = s[3] = s[4] = 0;
+    int64_t h[1] = {0};
+    for (int b = tid; b < B; b += NT) { const int64_t l = a.len0[b]; if (l >= 0 && l <= cap) h[0] += l / kTokens * 2; }
+    block_sums<1, NT>(h, red);
+    s[2] = h[0];
+  }
+  // decode: halves per item, four waves each a multiple of one half
+  const int dec_chunk = (int)max((int64_t)4, (s[2] + (int64_t)a.dec_items * 4 - 1) / ((int64_t)a.dec_items * 4) * 4);
+  const int pf_chunk = a.pf_items && s[3] * a.H_kv < kPfFill ? (int)max((int64_t)8, (s[4] + a.pf_items - 1) / a.pf_items) : 0x7fffffff;
+  int32_t carry[5] = {0, 0, 0, 0, 0};
+  for (int b0 = 0; b0 < B; b0 += NT) {
+    const int b = b0 + tid;
+    int l = 0, n = 0;
+    if (b < B) {
+      const int64_t ll = a.len0[b];
+      l = ll >= 0 && ll <= cap ? (int)ll : 0;
+      n = ok ? a.n_new[b] : 0;
+    }
+    const int t = l + n, f0 = l / kTokens, f1 = t / kTokens, halves = f1 * 2;
+    const int qb = (int)(((int64_t)n * G + kQCols - 1) / kQCols), seen = (t + 63) / 64;
+    int32_t v[5];
+    v[0] = n;
+    v[1] = n > 0 ? max(1, f1 - f0) : 0;
+    v[2] = (halves + dec_chunk - 1) / dec_chunk + (t % kTokens ? 1 : 0);
+    v[3] = qb * (seen ? (seen - 1) / pf_chunk + 1 : 0);
+    v[4] = f1 - f0;
+    int32_t inc[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      int x = v[i];
+      for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o, 64); if (lane >= o) x += y; }
+      inc[i] = x;
+      if (lane == 63) wsum[i][wave] = x;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      int before = carry[i];
+      for (int k = 0; k < NT / 64; ++k) { const int y = wsum[i][k]; if (k < wave) before += y; carry[i] += y; }
+      inc[i] += before;
+    }
+    __syncthreads();
+    if (b < B) {
+      a.plan.row_start()[b + 1] = inc[0]; a.plan.app()[b + 1] = inc[1]; a.plan.dec()[b + 1] = inc[2];
+      a.plan.pf()[b + 1] = inc[3]; a.plan.fresh()[b + 1] = inc[4];
+      a.plan.len()[b] = t;
+      a.len1[b] = ok ? t : a.len0[b];
+    }
+  }
+  if (tid == 0) {
+    int32_t* w = a.plan.w;
+    for (int i : {0, 2, 3, 4, 5}) a.plan.arr(i)[0] = 0;
+    w[kStatus] = status; w[kRows] = (int)s[0]; w[kDecChunk] = dec_chunk; w[kDecItems] = carry[2]; w[kPfChunk] = pf_chunk; w[kPfItems] = carry[3];
+    w[kAppItems] = carry[1]; w[kNewPages] = carry[4]; w[kFree0] = n_free0;
+    w[kBatch] = B; w[kHq] = a.H_q; w[kHkv] = a.H_kv; w[kMaxRows] = a.max_rows; w[kMagic] = kMagicWord;
+    *a.n_free1 = n_free0 - (ok ? (int)s[1] : 0);
+  }
+  if (!a.rows_here) return;
+  __syncthreads();                                     // (the plan's arrays: written by this workgroup, read by it)
+  __threadfence_block();
+  for (int row = tid; row < (int)s[0]; row += NT) {
+    const int b = find_seq(a.plan.row_start(), B, row);
+    const int r0 = a.plan.row_start()[b];
+    grow_row(a, row, b, r0, a.plan.len()[b], a.plan.row_start()[b + 1] - r0, a.plan.fresh()[b], n_free0);
+  }
+}
+
+__global__ __launch_bounds__(256) void grow_rows_kernel(GrowArgs a) {
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row >= a.plan.w[kRows]) return;
+  const int32_t* rs = a.plan.row_start();
+  const int b = find_seq(rs, a.plan.n, row);
+  grow_row(a, row, b, rs[b], a.plan.len()[b], rs[b + 1] - rs[b], a.plan.fresh()[b], a.plan.w[kFree0]);
+}
+
+// ---- slots of any cached tokens
+struct SlotArgs {
+  const int32_t *table, *len, *row_start, *first;
+  int32_t* slot;
+  int batch, max_pages, n_rows;
+};
+constexpr int32_t kNoSlot = (int32_t)0x80000000;
+__global__ __launch_bounds__(256) void slots_kernel(SlotArgs a) {
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row >= a.n_rows || row < a.row_start[0] || row >= a.row_start[a.batch]) return;
+  const int b = find_seq(a.row_start, a.batch, row);
+  const int64_t p = (int64_t)a.first[b] + row - a.row_start[b], len = a.len[b];
+  int32_t slot = kNoSlot;
+  if (p >= 0 && p < len && len / kTokens <= a.max_pages) {
+    if (p / kTokens < len / kTokens) {
+      const int page = a.table[(int64_t)b * a.max_pages + p / kTokens];
+      if (page >= 0) slot = (int32_t)((int64_t)page * kTokens + p % kTokens);
+    } else {
+      slot = -1 - (b * kTokens + (int)(p % kTokens));
+    }
+  }
+  a.slot[row] = slot;
+}
+
+// ---- pages of finished sequences back onto the stack, in the order of sequences and blocks
+struct ReleaseArgs {
+  const int32_t* which;
+  int32_t *table, *len, *free_list, *n_free;
+  int batch, max_pages, n_pages;
+};
+template <int NT>
+__global__ __launch_bounds__(NT) void release_kernel(ReleaseArgs a) {
+  __shared__ int32_t start[kMaxBatch + 1];
+  __shared__ int32_t wsum[NT / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = a.batch;
+  const int n0 = *a.n_free;
+  int64_t carry = 0;
+  for (int b0 = 0; b0 < B; b0 += NT) {
+    const int b = b0 + tid;
+    int x = 0;
+    if (b < B && a.which[b]) { const int l = a.len[b]; x = l < 0 ? 0 : min(l / kTokens, a.max_pages); }
+    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o, 64); if (lane >= o) x += y; }
+    if (lane == 63) wsum[wave] = x;
+    __syncthreads();
+    int64_t before = carry;
+    for (int k = 0; k < NT / 64; ++k) { if (k < wave) before += wsum[k]; carry += wsum[k]; }
+    if (b < B) start[b + 1] = (int32_t)min(before + x, (int64_t)0x7fffffff);
+    __syncthreads();
+  }
+  if (tid == 0) start[0] = 0;
+  __syncthreads();
+  if (n0 < 0 || carry > (int64_t)a.n_pages - n0) return;        // more pages than the pool has: released twice, nothing is touched
+  for (int i = tid; i < (int)carry; i += NT) {
+    const int b = find_seq(start, B, i);
+    int32_t* e = a.table + (int64_t)b * a.max_pages + (i - start[b]);
+    a.free_list[n0 + i] = *e;
+    *e = -1;
+  }
+  for (int b = tid; b < B; b += NT) if (a.which[b]) a.len[b] = 0;
+  if (tid == 0) *a.n_free = n0 + (int)carry;
+}
+
+// ---- rows into pages and tails
+struct StoreArgs {
+  uint8_t *k, *v, *ke, *ve;
+  bf16_t *kt, *vt;
+  const bf16_t *kn, *vn;
+  const int32_t* table;
+  Plan plan;
+  PlanKey key;
+  int max_pages, n_pages;
+};
+
+// Least power of two >= 2^kMinExp with amax <= 448 * 2^e, as its byte.  448 = 1.75 * 2^8; amax is a bf16 number.
+__device__ __forceinline__ int scale_byte(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  return max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 127 + kMinExp);
+}
+
+// One workgroup per (item, KV head).  Item 0 of a sequence also moves the rows behind its last full block into the tail, after it has read
+// the tail's old rows for the first block.
+template <int HD>
+__global__ __launch_bounds__(256) void append_kernel(StoreArgs a) {
+  constexpr int CPR = HD / 8, RPP = 256 / CPR, PASSES = kTokens / RPP;      // 16-byte chunks of a row, rows of a pass
+  __shared__ __attribute__((aligned(16))) uint8_t vbytes[kTokens * HD];
+  __shared__ float wmax[2][4];
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
+  if (!made_for(a.plan, a.key) || item >= a.plan.w[kAppItems]) return;
+  const int b = find_item(a.plan.app(), a.key.batch, item), j = item - a.plan.app()[b];
+  const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len1 = a.plan.len()[b], len0 = len1 - n;
+  const int f0 = len0 / kTokens, f1 = len1 / kTokens;
+  const int64_t D = (int64_t)a.key.H_kv * HD;
+  const int rr = tid / CPR, cc = tid % CPR;
+  bool odd = false;
+  const int64_t tail0 = (int64_t)b * kTokens * D + kvh * HD, new0 = (int64_t)row0 * D + kvh * HD;
+  if (f1 > f0) {
+    const int blk = f0 + j, page = a.table[(int64_t)b * a.max_pages + blk];
+    uint4 x[2][PASSES];
+    float m[2] = {0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int tok = p * RPP + rr, at = blk * kTokens + tok;
+      const int64_t o = cc * 8 + (at < len0 ? tail0 + tok * D : new0 + (int64_t)(at - len0) * D);
+      x[0][p] = *reinterpret_cast<const uint4*>((at < len0 ? a.kt : a.kn) + o);
+      x[1][p] = *reinterpret_cast<const uint4*>((at < len0 ? a.vt : a.vn) + o);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        x[s][p] = finite8(x[s][p], odd);
+        float f[8];
+        unpack_bf16x8(x[s][p], f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[s] = fmaxf(m[s], fabsf(f[i]));
+      }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      m[s] = wave_max64(m[s]);
+      if ((tid & 63) == 0) wmax[s][wave] = m[s];
+    }
+    __syncthreads();
+    int e[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) e[s] = scale_byte(fmaxf(fmaxf(wmax[s][0], wmax[s][1]), fmaxf(wmax[s][2], wmax[s][3])));
+    const bool good = (uint32_t)page < (uint32_t)a.n_pages;
+    const int64_t ph = (int64_t)page * a.key.H_kv + kvh;
+    uint8_t* kp = a.k + ph * (kTokens * HD);
+    uint8_t* vp = a.v + ph * (kTokens * HD);
+    const float down[2] = {exp_to_scale(254 - e[0]), exp_to_scale(254 - e[1])};      // 2^-e: e is within +-120
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        float f[8];
+        unpack_bf16x8(x[s][p], f);
+        uint2 c;
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * down[s], f[1] * down[s], 0, false);
+        c.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * down[s], f[3] * down[s], w, true);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4] * down[s], f[5] * down[s], 0, false);
+        c.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6] * down[s], f[7] * down[s], w, true);
+        const int tok = p * RPP + rr;
+        if (s == 0) {
+          if (good) *reinterpret_cast<uint2*>(kp + k_offset<HD>(tok, cc * 8)) = c;
+        } else {
+          *reinterpret_cast<uint2*>(vbytes + tok * HD + cc * 8) = c;
+        }
+      }
+    __syncthreads();
+    if (good) {
+      // a thread: four dims of 16 tokens (those of one lane group and half), four chunks whose bytes are the tokens'
+      for (int i = tid; i < HD / 4 * 8; i += 256) {
+        const int dq = i % (HD / 4), g = i / (HD / 4) % 4, h = i / (HD / 4) / 4;
+        uint32_t o[4][4];                              // [dim][tile]
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          uint32_t w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(vbytes + (h * 64 + t * 16 + g * 4 + k) * HD + dq * 4);
+          const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
+          const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+          o[0][t] = __builtin_amdgcn_perm(b0, a0, 0x05040100); o[1][t] = __builtin_amdgcn_perm(b0, a0, 0x07060302);
+          o[2][t] = __builtin_amdgcn_perm(b1, a1, 0x05040100); o[3][t] = __builtin_amdgcn_perm(b1, a1, 0x07060302);
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          *reinterpret_cast<uint4*>(vp + v_offset<HD>(h * 64 + g * 4, dq * 4 + d)) = make_uint4(o[d][0], o[d][1], o[d][2], o[d][3]);
+      }
+      if (tid == 0) { a.ke[ph] = (uint8_t)e[0]; a.ve[ph] = (uint8_t)e[1]; }
+    }
+  }
+  if (j == 0) {                                        // (its reads of the tail's old rows are behind the barriers above)
+    const int first = f1 > f0 ? f1 * kTokens : len0;
+    for (int i = tid; i < (len1 - first) * CPR; i += 256) {
+      const int p = first + i / CPR;
+      const int64_t src = new0 + (int64_t)(p - len0) * D + i % CPR * 8, dst = tail0 + (int64_t)(p % kTokens) * D + i % CPR * 8;
+      *reinterpret_cast<uint4*>(a.kt + dst) = finite8(*reinterpret_cast<const uint4*>(a.kn + src), odd);
+      *reinterpret_cast<uint4*>(a.vt + dst) = finite8(*reinterpret_cast<const uint4*>(a.vn + src), odd);
+    }
+  }
+  if (__any(odd) && (tid & 63) == 0) atomicOr(a.plan.w + kStatus, 16);            // ECHOKV_PLAN_NOT_FINITE
+}
+
+// ---- rows by their slots
+template <typename TO> struct ReadArgs {
+  const uint8_t *k, *v, *ke, *ve;
+  const bf16_t *kt, *vt;
+  const int32_t* slot;
+  TO *ko, *vo;
+  int n_rows, n_pages, batch, H_kv;
+};
+
+template <typename TO> __device__ __forceinline__ void put8(TO* p, uint4 b) {      // eight bf16 values
+  if constexpr (sizeof(TO) == 2) {
+    *reinterpret_cast<uint4*>(p) = b;
+  } else {
+    float f[8];
+    unpack_bf16x8(b, f);
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  }
+}
+
+// 128 rows of one KV head per workgroup.  A run of rows of one page goes through LDS, where the bytes of a value row lie 16 apart; shorter runs
+// than kLongRun rows, scattered rows and rows of tails are read where they are, all at once.
+constexpr int kLongRun = 16;
+template <int HD, typename TO>
+__global__ __launch_bounds__(256) void read_kernel(ReadArgs<TO> a) {
+  constexpr int CPR = HD / 8, BYTES = kTokens * HD;
+  __shared__ __attribute__((aligned(16))) uint8_t kb[BYTES], vb[BYTES];
+  __shared__ int32_t slots[kTokens];
+  const int tid = threadIdx.x, lane = tid & 63, kvh = blockIdx.x % a.H_kv, row0 = blockIdx.x / a.H_kv * kTokens, n = min(kTokens, a.n_rows - row0);
+  const int64_t D = (int64_t)a.H_kv * HD;
+  if (tid < n) slots[tid] = a.slot[row0 + tid];
+  __syncthreads();
+  // bit i: row i is of another page (or tail) than row i - 1; past the last row all bits are set
+  const auto differs = [&](int i) { return i >= n || i == 0 || (slots[i] >> 7) != (slots[i - 1] >> 7); };
+  const uint64_t edge[2] = {__ballot(differs(lane)), __ballot(differs(64 + lane))};
+  const auto run_end = [&](int i) {                       // first edge behind row i
+    const uint64_t lo = i < 63 ? edge[0] >> (i + 1) << (i + 1) : 0, hi = i < 64 ? edge[1] : i < 127 ? edge[1] >> (i - 63) << (i - 63) : 0;
+    return lo ? __ffsll((long long)lo) - 1 : hi ? 63 + __ffsll((long long)hi) : kTokens;
+  };
+  const auto run_start = [&](int i) {                     // last edge up to row i
+    const uint64_t hi = i < 64 ? 0 : edge[1] << (127 - i), lo = i < 64 ? edge[0] << (63 - i) : edge[0];
+    return hi ? i - __clzll((long long)hi) : (i < 64 ? i : 63) - __clzll((long long)lo);
+  };
+  const auto put_page_row = [&](const uint8_t* kp, const uint8_t* vp, float ks, float vs, int tok, int c, int64_t o) {
+    const uint2 kk = *reinterpret_cast<const uint2*>(kp + k_offset<HD>(tok, c));
+    const uint8_t* vv = vp + v_offset<HD>(tok, c);
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      w[h] = vv[64 * h] | (uint32_t)vv[64 * h + 16] << 8 | (uint32_t)vv[64 * h + 32] << 16 | (uint32_t)vv[64 * h + 48] << 24;
+    put8(a.ko + o, widen8(kk.x, kk.y, ks));
+    put8(a.vo + o, widen8(w[0], w[1], vs));
+  };
+  for (int x = tid; x < n * CPR; x += 256) {
+    const int i = x / CPR, c = x % CPR * 8, s = slots[i];
+    const int64_t o = (row0 + i) * D + kvh * HD + c;
+    if (s < 0) {
+      const int64_t t = -1 - (int64_t)s;
+      if (t >= (int64_t)a.batch * kTokens) continue;
+      put8(a.ko + o, *reinterpret_cast<const uint4*>(a.kt + t * D + kvh * HD + c));
+      put8(a.vo + o, *reinterpret_cast<const uint4*>(a.vt + t * D + kvh * HD + c));
+    } else if ((s >> 7) < a.n_pages && run_end(i) - run_start(i) < kLongRun) {
+      const int64_t ph = (int64_t)(s >> 7) * a.H_kv + kvh;
+      put_page_row(a.k + ph * BYTES, a.v + ph * BYTES, exp_to_scale(a.ke[ph]), exp_to_scale(a.ve[ph]), s & 127, c, o);
+    }
+  }
+  for (int i = 0; i < n;) {
+    const int end = __builtin_amdgcn_readfirstlane(min(n, run_end(i))), first = slots[i], page = first >> 7;
+    if (first >= 0 && page < a.n_pages && end - i >= kLongRun) {
+      const int64_t ph = (int64_t)page * a.H_kv + kvh;
+      const uint4* kp = reinterpret_cast<const uint4*>(a.k + ph * BYTES);
+      const uint4* vp = reinterpret_cast<const uint4*>(a.v + ph * BYTES);
+      const float ks = exp_to_scale(a.ke[ph]), vs = exp_to_scale(a.ve[ph]);
+      __syncthreads();                                    // the page before is read
+      for (int x = tid; x < BYTES / 16; x += 256) { reinterpret_cast<uint4*>(kb)[x] = kp[x]; reinterpret_cast<uint4*>(vb)[x] = vp[x]; }
+      __syncthreads();
+      for (int x = tid; x < (end - i) * CPR; x += 256) {
+        const int row = i + x / CPR, c = x % CPR * 8;
+        put_page_row(kb, vb, ks, vs, slots[row] & 127, c, (row0 + row) * D + kvh * HD + c);
+      }
+    }
+    i = end;
+  }
+}
+
+}  // namespace page
+}  // namespace echokv
