@@ -466,7 +466,8 @@ typedef struct {
 typedef struct {
   void *buf;          /* device, echokv_page_plan_bytes(batch) */
   size_t bytes;
-  int32_t max_rows;   /* new rows of a step at most (rows of k_new etc.), <= 2^30; 0: a plan for decode alone */
+  int32_t max_rows;   /* new rows of a step at most (rows of k_new etc.); times H_q / H_kv below 2^30;
+                         0: a plan for decode alone */
 } echokv_page_plan;
 #define ECHOKV_PLAN_BAD_LENGTH 1    /* a length, n_new or *n_free is negative or past its bound */
 #define ECHOKV_PLAN_TABLE_FULL 2    /* a sequence would pass max_pages full pages */

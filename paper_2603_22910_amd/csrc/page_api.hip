@@ -51,9 +51,10 @@ int check_cache(const echokv_page_cache* c) {
 
 size_t plan_bytes(int batch) { return ((page::kHeadWords + (size_t)page::Plan::kArrays * (batch + 1)) * 4 + 255) / 256 * 256; }
 
-int check_plan(const echokv_page_plan* p, int batch) {
+int check_plan(const echokv_page_plan* p, const Sizes& z, int batch) {
   if (!p || !p->buf) return ECHOKV_ERR_NULL;
   if (p->max_rows < 0 || p->max_rows > 1 << 30) return ECHOKV_ERR_SHAPE;
+  if ((int64_t)p->max_rows * z.G >= (int64_t)1 << 30) return ECHOKV_ERR_UNSUPPORTED;      // (query, query head) columns in 32 bits
   if (p->bytes < plan_bytes(batch) || !aligned16({p->buf})) return ECHOKV_ERR_WORKSPACE;
   return ECHOKV_OK;
 }
@@ -102,10 +103,12 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
 size_t part_bytes(int64_t rows, int d) { return (size_t)rows * (d + 2) * 4; }
 
 template <class F> int by_type(const Sizes& z, const page::AttnArgs& a, F f) {
-  const bool mods = a.cap > 0.f || a.slopes;
-  auto typed = [&](auto hd, auto md) { return z.out_bf16 ? f(hd, md, bf16_t{}) : f(hd, md, float{}); };
-  auto modded = [&](auto hd) { return mods ? typed(hd, std::true_type{}) : typed(hd, std::false_type{}); };
-  return z.d == 64 ? modded(std::integral_constant<int, 64>{}) : modded(std::integral_constant<int, 128>{});
+  auto typed = [&](auto hd, auto mode) { return z.out_bf16 ? f(hd, mode, bf16_t{}) : f(hd, mode, float{}); };
+  auto modal = [&](auto hd) {
+    if (a.cap > 0.f) return typed(hd, std::integral_constant<int, page::kCap>{});
+    return a.slopes ? typed(hd, std::integral_constant<int, page::kBias>{}) : typed(hd, std::integral_constant<int, page::kPlain>{});
+  };
+  return z.d == 64 ? modal(std::integral_constant<int, 64>{}) : modal(std::integral_constant<int, 128>{});
 }
 
 }  // namespace
@@ -116,7 +119,7 @@ size_t echokv_page_plan_bytes(int32_t batch) { return batch > 0 && batch <= page
 
 size_t echokv_page_workspace_bytes(const echokv_shape* shape, int32_t batch, int32_t max_rows) {
   Sizes z;
-  if (check_shape(shape, &z) || batch <= 0 || batch > page::kMaxBatch || max_rows < 0 || max_rows > 1 << 30) return 0;
+  if (check_shape(shape, &z) || batch <= 0 || batch > page::kMaxBatch || max_rows < 0 || (int64_t)max_rows * z.G >= (int64_t)1 << 30) return 0;
   const Schedule s = schedule(z, batch, max_rows);
   const size_t dec = part_bytes(s.dec_grid * z.H_q, z.d), pf = part_bytes(s.pf_parts * z.H_kv * page::kQCols, z.d);
   return (std::max(dec, pf) + 255) / 256 * 256;
@@ -127,7 +130,7 @@ int echokv_pages_grow(const echokv_shape* shape, const echokv_page_table* t, con
   Sizes z;
   int rc = check_shape(shape, &z);
   if (rc) return rc;
-  if ((rc = check_table(t)) || (rc = check_plan(plan, t->batch))) return rc;
+  if ((rc = check_table(t)) || (rc = check_plan(plan, z, t->batch))) return rc;
   if (!n_new || !seq_len_out || !n_free_out) return ECHOKV_ERR_NULL;
   const Schedule s = schedule(z, t->batch, plan->max_rows);
   page::GrowArgs a;
@@ -176,7 +179,7 @@ int echokv_page_append(const echokv_shape* shape, const echokv_page_table* t, co
   Sizes z;
   int rc = check_shape(shape, &z);
   if (rc) return rc;
-  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, t->batch))) return rc;
+  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, z, t->batch))) return rc;
   if (plan->max_rows == 0) return ECHOKV_OK;
   if (!k_new || !v_new) return ECHOKV_ERR_NULL;
   if (!aligned16({k_new, v_new})) return ECHOKV_ERR_SHAPE;
@@ -226,7 +229,7 @@ int echokv_page_decode_attn(const echokv_shape* shape, const echokv_page_table* 
   Sizes z;
   int rc = check_shape(shape, &z);
   if (rc) return rc;
-  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, t->batch))) return rc;
+  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, z, t->batch))) return rc;
   const Schedule s = schedule(z, t->batch, plan->max_rows);
   page::AttnArgs a;
   if ((rc = attn_args(z, t, c, plan, q, extras, out, lse_out, s, &a))) return rc;
@@ -236,10 +239,10 @@ int echokv_page_decode_attn(const echokv_shape* shape, const echokv_page_table* 
   a.part_ml = a.part_o + rows * z.d;
   dim3 grid, merge;
   if ((rc = launch_dims(s.dec_grid * z.H_kv * s.col_tiles, 256, &grid)) || (rc = launch_dims((int64_t)t->batch * z.H_q, 256, &merge))) return rc;
-  return by_type(z, a, [&](auto hd, auto md, auto to) -> int {
+  return by_type(z, a, [&](auto hd, auto mode, auto to) -> int {
     constexpr int HD = decltype(hd)::value;
     using TO = decltype(to);
-    hipLaunchKernelGGL((page::decode_kernel<HD, decltype(md)::value, TO>), grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+    hipLaunchKernelGGL((page::decode_kernel<HD, decltype(mode)::value, TO>), grid, dim3(256), 0, (hipStream_t)hip_stream, a);
     LAUNCH_CHECK();
     hipLaunchKernelGGL((page::decode_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a);
     LAUNCH_CHECK();
@@ -253,7 +256,7 @@ int echokv_page_prefill_attn(const echokv_shape* shape, const echokv_page_table*
   Sizes z;
   int rc = check_shape(shape, &z);
   if (rc) return rc;
-  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, t->batch))) return rc;
+  if ((rc = check_table(t)) || (rc = check_cache(c)) || (rc = check_plan(plan, z, t->batch))) return rc;
   if (plan->max_rows == 0) return ECHOKV_OK;
   const Schedule s = schedule(z, t->batch, plan->max_rows);
   page::AttnArgs a;
@@ -265,10 +268,10 @@ int echokv_page_prefill_attn(const echokv_shape* shape, const echokv_page_table*
   dim3 grid, merge;
   if ((rc = launch_dims(s.pf_grid * z.H_kv, page::kPfThreads, &grid)) || (rc = launch_dims(s.pf_parts * z.H_kv, 256, &merge))) return rc;
   merge.y = page::kQCols / 16;
-  return by_type(z, a, [&](auto hd, auto md, auto to) -> int {
+  return by_type(z, a, [&](auto hd, auto mode, auto to) -> int {
     constexpr int HD = decltype(hd)::value;
     using TO = decltype(to);
-    hipLaunchKernelGGL((page::prefill_kernel<HD, decltype(md)::value, TO>), grid, dim3(page::kPfThreads), 0, (hipStream_t)hip_stream, a);
+    hipLaunchKernelGGL((page::prefill_kernel<HD, decltype(mode)::value, TO>), grid, dim3(page::kPfThreads), 0, (hipStream_t)hip_stream, a);
     LAUNCH_CHECK();
     if (s.pf_parts) {
       hipLaunchKernelGGL((page::prefill_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a);

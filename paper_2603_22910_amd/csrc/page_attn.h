@@ -45,42 +45,57 @@ template <class F> __device__ __forceinline__ float across_rows(float v, F f) {
 __device__ __forceinline__ float rows_max(float v) { return across_rows(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float rows_sum(float v) { return across_rows(v, [](float a, float b) { return a + b; }); }
 
-// Raw products to scores in base 2.  cap: c tanh(s / c); where all of a wave's arguments are small by the odd series, of which the terms past
-// x^9 are below 2^-25 of the first, else by 1 - 2 / (1 + e^2x), whose error is half a step of one, 2^-24 of the cap.
-struct Mods { float scale2, cap2, to_arg, slope2; };
-template <int N> __device__ __forceinline__ void score(float (&s)[N], const Mods& m, bool mods, float away0, const int (&step)[N]) {
-  if (!mods) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] *= m.scale2;
-    return;
-  }
-  if (m.cap2 > 0.f) {
+// What is done to the raw products: nothing but a factor, which is left to the exponent's fused multiply-add; a bias; a cap, and maybe a bias.
+enum { kPlain, kBias, kCap };
+struct Mods { float scale2, cap2, to_arg; };
+template <int MODE> __device__ __forceinline__ float factor(const Mods& m) { return MODE == kPlain ? m.scale2 : 1.f; }
+__device__ __forceinline__ Mods mods_of(const AttnArgs& a) { return {a.scale * kLog2e, a.cap * kLog2e, a.cap > 0.f ? a.scale / a.cap : 0.f}; }
+
+// Raw products of C columns to scores in base 2.  c tanh(s / c): where all of a wave's arguments are small by the odd series, of which the terms past
+// x^9 are below 2^-25 of the first, else by (1 - e) / (1 + e), e = e^-2x, whose error is half a step of one, 2^-24 of the cap.
+// slope2[c]: slope in base 2; away[c]: key minus query position at the lane's first key, at[i] keys before the i-th.
+template <int MODE, int C, int N>
+__device__ __forceinline__ void score(float (&s)[C][N], const Mods& m, const float (&slope2)[C], const float (&away)[C], const int (&at)[N]) {
+  if constexpr (MODE == kCap) {
     float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) { s[i] *= m.to_arg; top = fmaxf(top, fabsf(s[i])); }
-    if (__any(!(top < 0.2f))) {
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float e = __builtin_amdgcn_exp2f(fabsf(s[i]) * (-2.f * kLog2e));          // (towards zero from either side: no overflow)
-        s[i] = copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), s[i]) * m.cap2;
+      for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(s[c][i]));
+    if (__any(!(top * m.to_arg < 0.2f))) {
+      const float arg2 = m.to_arg * (-2.f * kLog2e);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float e = __builtin_amdgcn_exp2f(fabsf(s[c][i]) * arg2);        // (towards zero from either side: no overflow)
+          s[c][i] = copysignf((m.cap2 - m.cap2 * e) * __builtin_amdgcn_rcpf(1.f + e), s[c][i]);
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (four at a time: more take more registers than there are)
+        }
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float x2 = s[i] * s[i];
-        const float t = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-        s[i] = s[i] * t * m.cap2;
+      for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float x = s[c][i] * m.to_arg, x2 = x * x;
+          s[c][i] = x * m.cap2 * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] *= m.scale2;
   }
+  if constexpr (MODE != kPlain) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) s[i] = fmaf(m.slope2, away0 + (float)step[i], s[i]);
-}
-__device__ __forceinline__ Mods mods_of(const AttnArgs& a, float slope) {
-  return {a.scale * kLog2e, a.cap * kLog2e, a.cap > 0.f ? a.scale / a.cap : 0.f, slope * kLog2e};
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float x = MODE == kCap ? s[c][i] : s[c][i] * m.scale2;
+        s[c][i] = fmaf(slope2[c], away[c] + (float)at[i], x);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
 }
 
 template <typename TO> __device__ __forceinline__ void put4(TO* p, float4 v) {
@@ -93,7 +108,7 @@ template <typename TO> __device__ __forceinline__ void put4(TO* p, float4 v) {
 // joined in LDS.  What bounds it is the reading of the pages.
 constexpr int kDecodeItems = 1024;      // workgroups that the pages of a launch are shared out to
 
-template <int HD, bool MODS, typename TO>
+template <int HD, int MODE, typename TO>
 __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
   constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16;
   __shared__ __attribute__((aligned(16))) float so[4][16][HD + 4];
@@ -110,7 +125,8 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
   uint4 qf[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
-  const Mods md = mods_of(a, MODS && a.slopes ? a.slopes[head] : 0.f);
+  const Mods md = mods_of(a);
+  const float fac = factor<MODE>(md), slope2[1] = {MODE != kPlain && a.slopes ? a.slopes[head] * kLog2e : 0.f};
 
   floatx4_t o[U];
 #pragma unroll
@@ -134,7 +150,7 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) vr[u] = vp[u * 64];
       const float ks = exp_to_scale(a.ke[ph]), vs = exp_to_scale(a.ve[ph]);
-      float s[16];
+      float s1[1][16], (&s)[16] = s1[0];
       int step[16];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -147,11 +163,11 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { s[4 * t + i] = acc[i]; step[4 * t + i] = 16 * t + i; }
       }
-      score(s, md, MODS, (float)(hf * 64 + 4 * g - (len - 1)), step);
+      score<MODE>(s1, md, slope2, {(float)(hf * 64 + 4 * g - (len - 1))}, step);
       float top = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      top = rows_max(top);
+      top = rows_max(top) * fac;
       if (__any(top > m)) {
         const float up = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - up);
         m = up;
@@ -162,7 +178,7 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
       uint32_t hi[8], lo[8];
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[i] - m), p1 = __builtin_amdgcn_exp2f(s[i + 1] - m);
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[i], fac, -m)), p1 = __builtin_amdgcn_exp2f(fmaf(s[i + 1], fac, -m));
         l += p0 + p1;
         hi[i / 2] = pack_bf16(p0, p1);
         lo[i / 2] = pack_bf16(p0 - __uint_as_float(hi[i / 2] << 16), p1 - __uint_as_float(hi[i / 2] & 0xffff0000u));
@@ -183,7 +199,7 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
     const int rows = len % kTokens, t0 = wave * 32;
     if (t0 < rows) {
       const int64_t D = (int64_t)a.key.H_kv * HD, base = (int64_t)b * kTokens * D + kvh * HD;
-      float s[8];
+      float s1[1][8], (&s)[8] = s1[0];
       int step[8];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -194,18 +210,18 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { s[4 * t + i] = acc[i]; step[4 * t + i] = 16 * t + i; }
       }
-      score(s, md, MODS, (float)(t0 + 4 * g - (rows - 1)), step);
-      float top = kNoScore;
+      score<MODE>(s1, md, slope2, {(float)(t0 + 4 * g - (rows - 1))}, step);
+      float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (t0 + 4 * g + step[i] >= rows) s[i] = -INFINITY;
         top = fmaxf(top, s[i]);
       }
-      m = rows_max(top);
+      m = rows_max(top) * fac;
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[i] - m), p1 = __builtin_amdgcn_exp2f(s[i + 1] - m);
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[i], fac, -m)), p1 = __builtin_amdgcn_exp2f(fmaf(s[i + 1], fac, -m));
         l += p0 + p1;
         hi[i / 2] = pack_bf16(p0, p1);
         lo[i / 2] = pack_bf16(p0 - __uint_as_float(hi[i / 2] << 16), p1 - __uint_as_float(hi[i / 2] & 0xffff0000u));
@@ -317,11 +333,37 @@ constexpr int kPfWaves = 8, kPfThreads = 64 * kPfWaves, kColTiles = kQCols / kPf
 constexpr int kPfShares = 512;           // workgroups that too few blocks of queries are split into
 constexpr float kRaise = 8.f;           // the reference of a softmax is raised once the maximum has passed it by 2^8: sums and outputs hold that
 
-template <int HD, bool MODS, typename TO>
+// The same number, of which the compiler knows nothing: what depends on it stays where it is used (out of a loop's registers).
+__device__ __forceinline__ int opaque(int x) { asm volatile("" : "+v"(x)); return x; }
+
+// Products with N operands that lie in LDS one KB apart, in order; operand n is requested four products' operands ahead (its latency is that of three
+// to four groups of products, and what the compiler would choose is the order that takes the fewest registers).
+template <int N, class F> __device__ __forceinline__ void with_operands(const uint4* p, F f) {
+  constexpr int A = 4;
+  uint4 x[A];
+#pragma unroll
+  for (int n = 0; n < A; ++n) x[n] = p[n * 64];
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    f(n, x[n % A]);
+    if (n + A < N) x[n % A] = p[(n + A) * 64];
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// Own LDS operations done, then the workgroup's barrier; loads from memory stay in flight.
+__device__ __forceinline__ void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);                                   // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int HD, int MODE, typename TO>
 __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
   constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16, CT = kColTiles;
-  constexpr int KFRAGS = 4 * KS, VFRAGS = 2 * U, NCH = HD / 64;      // 1 KB operands of a half; 16-byte chunks of codes a thread moves
-  __shared__ __attribute__((aligned(16))) uint4 lds[2][(KFRAGS + VFRAGS) * 64];
+  __shared__ __attribute__((aligned(16))) uint4 kbuf[2][4 * KS * 64], vbuf[2][2 * U * 64];      // halves as operands of 1 KB
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   if (!made_for(a.plan, a.key)) return;
   const int n_items = a.plan.w[kPfItems];
@@ -331,166 +373,214 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
   const int b = find_item(a.plan.pf(), B, item), item0 = a.plan.pf()[b];
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
   const int chunk = a.plan.w[kPfChunk], shares = ((len + 63) / 64 - 1) / chunk + 1;
-  const int64_t cols = (int64_t)n * G;
-  const int blocks = (int)((cols + kQCols - 1) / kQCols), j = item - item0, share = j % shares;
-  const int64_t x0 = (int64_t)(blocks - 1 - j / shares) * kQCols;    // the longest ones first
+  const int cols = n * G;                   // (below 2^31: the host sees to it)
+  const int blocks = (cols - 1) / kQCols + 1, j = item - item0, share = j % shares;
+  const int x0 = (blocks - 1 - j / shares) * kQCols;    // the longest ones first
   const int prefix = a.prefix ? min(max(a.prefix[b], 0), len) : 0;
   const int full_halves = len / kTokens * 2, tail_rows = len % kTokens;
   // what the block and the wave see: keys up to their last column's own, or the prefix
-  const int64_t xl = min(x0 + kQCols, cols) - 1;
-  const int seen = max(len0 + (int)(xl / G) + 1, prefix);
+  const int xl = min(x0, cols - kQCols) + kQCols - 1;
+  const int seen = max(len0 + xl / G + 1, prefix);
   const int h0 = share * min(chunk, 0x3fffffff), h1 = min((seen + 63) / 64, shares > 1 ? h0 + chunk : 0x7fffffff);
-  const int64_t w0 = x0 + wave * (16 * CT);
+  const int w0 = min(x0 + wave * (16 * CT), cols);      // (cols: none of the wave's columns exists)
   const bool active = w0 < cols;
-  const int wave_first = len0 + (int)(min(w0, cols - 1) / G);         // position of the wave's first column
-  const int wave_seen = active ? max(len0 + (int)(min(w0 + 16 * CT, cols) - 1) / G + 1, prefix) : 0;
+  const int wave_first = len0 + min(w0, cols - 1) / G;         // position of the wave's first column
+  const int wave_seen = active ? max(len0 + (min(w0, cols - 16 * CT) + 16 * CT - 1) / G + 1, prefix) : 0;
 
   uint4 qf[CT][KS];
   int pos[CT];
-  float m[CT], l[CT], slope[CT];
+  float m[CT], l[CT], slope2[CT];
   floatx4_t o[CT][U];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
-    const int64_t x = min(w0 + 16 * c + r, cols - 1);
-    const int qi = (int)(x / G), head = kvh * G + (int)(x - (int64_t)qi * G);
+    const int x = min(w0, cols - 1 - (16 * c + r)) + 16 * c + r;         // the last column again past the end
+    const int qi = x / G, head = kvh * G + x - qi * G;
     pos[c] = len0 + qi;
     const bf16_t* qp = a.q + ((int64_t)(row0 + qi) * H_q + head) * HD + 8 * g;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[c][s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
-    slope[c] = MODS && a.slopes ? a.slopes[head] : 0.f;
+    slope2[c] = MODE != kPlain && a.slopes ? a.slopes[head] * kLog2e : 0.f;
     m[c] = kNoScore; l[c] = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) o[c][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   }
-  Mods md = mods_of(a, 0.f);
+  const Mods md = mods_of(a);
+  const float fac = factor<MODE>(md);
 
   const int32_t* pages = a.table + (int64_t)b * a.max_pages;
   const int64_t D = (int64_t)a.key.H_kv * HD, tail = (int64_t)b * kTokens * D + kvh * HD;
-  uint4 raw[NCH];
-  float scale[2] = {0.f, 0.f};
-  // a thread's 16-byte chunks: one of the keys and one of the values (HD = 128), or one of either by half of the threads
-  const auto fetch = [&](int hf) {
-    if (hf >= full_halves) return;
-    const int page = pages[hf >> 1];
-    const bool good = (uint32_t)page < (uint32_t)a.n_pages;
-    const int64_t ph = (int64_t)(good ? page : 0) * a.key.H_kv + kvh;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const bool val = KC == 2 ? i == 1 : tid >= 256;
-      raw[i] = reinterpret_cast<const uint4*>((val ? a.v : a.k) + ph * (kTokens * HD) + (hf & 1) * (64 * HD))[KC == 2 ? tid : tid & 255];
-    }
-    scale[0] = exp_to_scale(a.ke[ph]); scale[1] = exp_to_scale(a.ve[ph]);
+  // What a thread moves of a half: chunks of codes, of the keys by all threads or half of them, of the values by all or the others.  The codes are
+  // in registers a step before their place in LDS is free.
+  constexpr int KTHREADS = 256 * KC, VOFF = KTHREADS % kPfThreads;
+  const bool has_k = tid < KTHREADS, has_v = tid >= VOFF;
+  const int vtid = tid - VOFF;
+  uint4 kraw, vraw;
+  float kscale = 0.f, vscale = 0.f;
+  // Pages and scales come through the scalar cache during the softmax: in the products' phase they would be waited for together with the operands' LDS
+  // reads, which then could not run ahead.  -1: no page, or none of the pool
+  const auto page_of = [&](int hf) {
+    if (hf >= min(h1, full_halves)) return -1;
+    const int page = scalar_word(pages + (hf >> 1));
+    return (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
   };
-  const auto place = [&](int hf, uint4* buf) {
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const bool val = KC == 2 ? i == 1 : tid >= 256;
-      const int id = KC == 2 ? tid : tid & 255, cl = id & 63, cf = id >> 6, cr = cl & 15, cg = cl >> 4;
-      uint4 x0, x1;
-      if (hf < full_halves) {
-        const float sc = val ? scale[1] : scale[0];
-        x0 = widen8(raw[i].x, raw[i].y, sc); x1 = widen8(raw[i].z, raw[i].w, sc);
-      } else {
-        const int first = (hf - full_halves) * 64;
-        x0 = x1 = make_uint4(0, 0, 0, 0);
-        if (!val) {
-          const int tok = first + 16 * (cf / KC) + cr;
-          if (tok < tail_rows) {
-            const bf16_t* p = a.kt + tail + tok * D + 64 * (cf % KC) + 8 * cg;
-            x0 = *reinterpret_cast<const uint4*>(p); x1 = *reinterpret_cast<const uint4*>(p + 32);
-          }
-        } else {
-          uint32_t w[8];
-#pragma unroll
-          for (int y = 0; y < 16; ++y) {
-            const int tok = first + 16 * (y / 4) + 4 * cg + y % 4;
-            const uint32_t e = tok < tail_rows ? a.vt[tail + tok * D + 16 * cf + cr] : 0;
-            w[y / 2] = y % 2 ? w[y / 2] | e << 16 : e;
-          }
-          x0 = make_uint4(w[0], w[1], w[2], w[3]); x1 = make_uint4(w[4], w[5], w[6], w[7]);
-        }
+  const auto head_of = [&](int page) { return (int64_t)max(page, 0) * a.key.H_kv + kvh; };
+  const auto fetch_k = [&](int hf, int page) {
+    if (hf < min(h1, full_halves) && has_k) kraw = reinterpret_cast<const uint4*>(a.k + head_of(page) * (kTokens * HD) + (hf & 1) * (64 * HD))[tid];
+  };
+  const auto fetch_v = [&](int hf, int page) {
+    if (hf < min(h1, full_halves) && has_v) vraw = reinterpret_cast<const uint4*>(a.v + head_of(page) * (kTokens * HD) + (hf & 1) * (64 * HD))[vtid];
+  };
+  const auto place_k = [&](int hf) {
+    if (hf >= h1 || !has_k) return;
+    uint4 x0, x1;
+    int id = tid;
+    if (hf < full_halves) {
+      x0 = widen8(kraw.x, kraw.y, kscale); x1 = widen8(kraw.z, kraw.w, kscale);
+    } else {
+      id = opaque(tid);
+      const int cl = id & 63, cf = id >> 6;
+      const int tok = (hf - full_halves) * 64 + 16 * (cf / KC) + (cl & 15);
+      x0 = x1 = make_uint4(0, 0, 0, 0);
+      if (tok < tail_rows) {
+        const bf16_t* p = a.kt + tail + tok * D + 64 * (cf % KC) + 8 * (cl >> 4);
+        x0 = *reinterpret_cast<const uint4*>(p); x1 = *reinterpret_cast<const uint4*>(p + 32);
       }
-      uint4* f = buf + (val ? KFRAGS + 2 * cf : 2 * cf) * 64 + cl;
-      f[0] = x0; f[64] = x1;
+    }
+    uint4* f = kbuf[(hf - h0) & 1] + (id & ~63) + id;      // operands 2 cf and 2 cf + 1 of 64 lanes
+    f[0] = x0; f[64] = x1;
+  };
+  const auto place_v = [&](int hf) {
+    if (hf >= h1 || !has_v) return;
+    if (hf < full_halves) {
+      uint4* f = vbuf[(hf - h0) & 1] + (vtid & ~63) + vtid;
+      f[0] = widen8(vraw.x, vraw.y, vscale); f[64] = widen8(vraw.z, vraw.w, vscale);
+    } else {
+      const int id = opaque(vtid), cl = id & 63, cf = id >> 6;
+      uint16_t* f = reinterpret_cast<uint16_t*>(vbuf[(hf - h0) & 1] + 2 * cf * 64 + cl);
+      const int tok0 = (hf - full_halves) * 64 + 4 * (cl >> 4);
+#pragma unroll 1
+      for (int y = 0; y < 16; ++y) {
+        const int tok = tok0 + 16 * (y / 4) + y % 4;
+        f[(y / 8) * 512 + y % 8] = tok < tail_rows ? a.vt[tail + tok * D + 16 * cf + (cl & 15)] : 0;
+      }
     }
   };
 
-  if (h0 < h1) { fetch(h0); place(h0, lds[0]); }
-  __syncthreads();
-  for (int hf = h0; hf < h1; ++hf) {
-    const uint4* buf = lds[(hf - h0) & 1];
-    const bool more = hf + 1 < h1;
-    if (more) fetch(hf + 1);
+  uint4 pf[CT][2];
+  int page0 = page_of(h0), page1 = page_of(h0 + 1), page2 = page_of(h0 + 2);      // of this half and the next two
+  bool have = false;                      // probabilities of the half before
+  // A step: products (values of the half before, keys of this one), barrier, softmax, barrier.  Waves 4 .. 7 run one barrier behind, so that of the two
+  // waves of a SIMD one has the matrix pipe while the other has the vector unit.
+  const auto step = [&](int hf) {
+    __builtin_amdgcn_s_setprio(1);
+    const auto stage = [&](int part) {
+      if (part == 0) { place_k(hf + 1); fetch_k(hf + 2, page2); }
+      if (part == 1) { place_v(hf); fetch_v(hf + 1, page1); }
+    };
+    if (have) {
+      with_operands<2 * U>(vbuf[(hf - 1 - h0) & 1] + lane, [&](int n, const uint4& f) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[c][n / 2] = mfma(f, pf[c][n % 2], o[c][n / 2]);
+        if (n == 1) stage(0);                          // (in the shadow of the products)
+        if (n == 4) stage(1);
+      });
+    } else {
+      stage(0);
+      stage(1);
+    }
     const int first = hf * 64;
     // (a page outside the pool: its tokens are seen by nobody)
-    if (first < wave_seen && (hf >= full_halves || (uint32_t)pages[hf >> 1] < (uint32_t)a.n_pages)) {
-      floatx4_t s[CT][4];
+    have = hf < h1 && first < wave_seen && (hf >= full_halves || page0 >= 0);
+    floatx4_t s[CT][4];
+    if (have)
+      with_operands<4 * KS>(kbuf[(hf - h0) & 1] + lane, [&](int n, const uint4& f) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-#pragma unroll
-        for (int c = 0; c < CT; ++c) s[c][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const uint4 f = buf[(t * KS + k) * 64 + lane];
-#pragma unroll
-          for (int c = 0; c < CT; ++c) s[c][t] = mfma(f, qf[c][k], s[c][t]);
-        }
-      }
+        for (int c = 0; c < CT; ++c) s[c][n / KS] = mfma(f, qf[c][n % KS], n % KS ? s[c][n / KS] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+      });
+    barrier();
+    __builtin_amdgcn_s_setprio(0);
+    kscale = exp_to_scale(scalar_byte(a.ke + head_of(page2)));
+    vscale = exp_to_scale(scalar_byte(a.ve + head_of(page1)));
+    const int next = scalar_word(pages + (max(min(hf + 3, full_halves - 1), 0) >> 1));
+    if (have) {
       const bool masked = first + 63 > wave_first && first + 63 >= prefix;
-      uint4 pf[CT][2];
+      float v[CT][16], top[CT];
+      int at[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) at[i] = 16 * (i / 4) + i % 4;
+      float away[CT];
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        float v[16];
-        int step[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { v[i] = s[c][i / 4][i % 4]; step[i] = 16 * (i / 4) + i % 4; }
-        md.slope2 = slope[c] * kLog2e;
-        score(v, md, MODS, (float)(first + 4 * g - pos[c]), step);
+        for (int i = 0; i < 16; ++i) v[c][i] = s[c][i / 4][i % 4];
+        away[c] = (float)(first + 4 * g - pos[c]);
+      }
+      score<MODE>(v, md, slope2, away, at);
+      bool higher = false;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
         if (masked) {
           const int lim = max(pos[c], prefix - 1) - first - 4 * g;      // (the last key seen, from this lane's first)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = step[i] <= lim ? v[i] : -INFINITY;
+          for (int i = 0; i < 16; ++i) v[c][i] = at[i] <= lim ? v[c][i] : -INFINITY;
         }
-        float top = v[0];
+        top[c] = v[c][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, v[i]);
-        top = rows_max(top);
-        if (__any(top > m[c] + kRaise)) {
-          const float up = fmaxf(m[c], top), f = __builtin_amdgcn_exp2f(m[c] - up);
+        for (int i = 1; i < 16; ++i) top[c] = fmaxf(top[c], v[c][i]);
+        top[c] = rows_max(top[c]) * fac;
+        higher |= top[c] > m[c] + kRaise;
+      }
+      if (__any(higher)) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const float up = fmaxf(m[c], top[c]), f = __builtin_amdgcn_exp2f(m[c] - up);
           m[c] = up;
           l[c] *= f;
 #pragma unroll
           for (int u = 0; u < U; ++u) o[c][u] *= f;
         }
+      }
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
         uint32_t p[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(v[i] - m[c]), p1 = __builtin_amdgcn_exp2f(v[i + 1] - m[c]);
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(v[c][i], fac, -m[c])), p1 = __builtin_amdgcn_exp2f(fmaf(v[c][i + 1], fac, -m[c]));
           l[c] += p0 + p1;
           p[i / 2] = pack_bf16(p0, p1);      // one rounding of the probabilities, the matrix pipe's operand: 2^-9 of each, of either sign
         }
         pf[c][0] = make_uint4(p[0], p[1], p[2], p[3]); pf[c][1] = make_uint4(p[4], p[5], p[6], p[7]);
       }
+    } else {                              // (they do not live on through the products with the keys)
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint4 f = buf[(KFRAGS + 2 * u + k) * 64 + lane];
-#pragma unroll
-          for (int c = 0; c < CT; ++c) o[c][u] = mfma(f, pf[c][k], o[c][u]);
-        }
+      for (int c = 0; c < CT; ++c) pf[c][0] = pf[c][1] = make_uint4(0, 0, 0, 0);
     }
-    if (more) place(hf + 1, lds[(hf + 1 - h0) & 1]);
-    __syncthreads();
+    page0 = page1; page1 = page2;
+    page2 = hf + 3 < min(h1, full_halves) && (uint32_t)next < (uint32_t)a.n_pages ? next : -1;
+    barrier();
+  };
+  if (h0 < h1) {
+    fetch_k(h0, page0);
+    fetch_v(h0, page0);
+    kscale = exp_to_scale(scalar_byte(a.ke + head_of(page0)));
+    vscale = exp_to_scale(scalar_byte(a.ve + head_of(page0)));
+    place_k(h0);
+    fetch_k(h0 + 1, page1);
+    kscale = exp_to_scale(scalar_byte(a.ke + head_of(page1)));
+    __builtin_amdgcn_s_waitcnt(0x0F70);                                 // vmcnt(0): no load of the queries is waited for inside the loop
+    barrier();
+    if (wave >= 4) barrier();
+    for (int hf = h0; hf <= h1; ++hf) step(hf);       // (the last step adds the last half's values and nothing else)
+    if (wave < 4) barrier();
   }
 
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     const float sum = rows_sum(l[c]);
-    const int64_t x = w0 + 16 * c + r;
-    if (x >= cols) continue;
-    const int qi = (int)(x / G);
-    const int64_t row = (int64_t)(row0 + qi) * H_q + kvh * G + (x - (int64_t)qi * G);
+    const int off = 16 * c + opaque(r);
+    if (off >= cols - w0) continue;
+    const int x = w0 + off, qi = x / G;
+    const int64_t row = (int64_t)(row0 + qi) * H_q + kvh * G + (x - qi * G);
     if (shares == 1) {
       const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
@@ -517,12 +607,12 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a) {
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b];
   const int shares = ((len + 63) / 64 - 1) / a.plan.w[kPfChunk] + 1;
   if (shares == 1 || j % shares) return;
-  const int64_t cols = (int64_t)n * a.G;
-  const int64_t x0 = ((cols + kQCols - 1) / kQCols - 1 - j / shares) * kQCols;
+  const int cols = n * a.G;
+  const int x0 = ((cols - 1) / kQCols - j / shares) * kQCols;
   const int d4 = threadIdx.x % L * 4;
   for (int c = blockIdx.y * 16 + threadIdx.x / L; c < blockIdx.y * 16 + 16; c += ROWS) {
-    const int64_t x = x0 + c;
-    if (x >= cols) break;
+    if (c >= cols - x0) break;
+    const int x = x0 + c;
     const int64_t part = ((int64_t)item * a.key.H_kv + kvh) * kQCols + c, stride = (int64_t)a.key.H_kv * kQCols;
     float M = kNoScore;
     for (int i = 0; i < shares; ++i) M = fmaxf(M, a.part_ml[(part + i * stride) * 2]);
@@ -535,8 +625,8 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a) {
       sum = fmaf(f, ml.y, sum);
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y); acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
     }
-    const int qi = (int)(x / a.G);
-    const int64_t row = (int64_t)(row0 + qi) * a.key.H_q + kvh * a.G + (x - (int64_t)qi * a.G);
+    const int qi = x / a.G;
+    const int64_t row = (int64_t)(row0 + qi) * a.key.H_q + kvh * a.G + (x - qi * a.G);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     put4(reinterpret_cast<TO*>(a.out) + row * HD + d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
     if (a.lse && d4 == 0) a.lse[row] = sum > 0.f ? (M + __log2f(sum)) * kLn2 : -INFINITY;

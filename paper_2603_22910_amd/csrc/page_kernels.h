@@ -53,6 +53,15 @@ __device__ __forceinline__ int find_item(const int32_t* start, int n, int x) {
   return __builtin_amdgcn_readfirstlane(at);
 }
 
+// A word that no kernel of this launch writes, at an address that all lanes share: through the scalar cache, so that it takes no vector register and
+// no place among the vector loads that are waited for in order.
+__device__ __forceinline__ int32_t scalar_word(const int32_t* p) { return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p; }
+// The same for a byte.
+__device__ __forceinline__ int scalar_byte(const uint8_t* p) {
+  const uintptr_t u = (uintptr_t)p;
+  return (scalar_word((const int32_t*)(u & ~(uintptr_t)3)) >> (8 * (u & 3))) & 0xff;
+}
+
 // ---- page layout, byte offsets inside one head's 128 * d
 // Keys: 16-byte chunk of a lane (r = token % 16, g) of the 16-token tile t: dims 8 g .. 8 g + 7 of two 32-dim steps of the product.
 template <int HD> __device__ __forceinline__ int k_offset(int token, int dim) {

@@ -117,6 +117,7 @@ def test_caches(name):
 
 
 @pytest.mark.parametrize("change,want", [(dict(buf=None), ek.ERR_NULL), (dict(max_rows=-1), ek.ERR_SHAPE), (dict(max_rows=(1 << 30) + 1), ek.ERR_SHAPE),
+                                         (dict(max_rows=1 << 28), ek.ERR_UNSUPPORTED),
                                          (dict(bytes=64), ek.ERR_WORKSPACE), (dict(buf=FAKE + 4), ek.ERR_WORKSPACE)])
 def test_plans(change, want):
     names = ("grow", "append", "decode", "prefill")
