@@ -61,19 +61,25 @@ int check_plan(const echokv_page_plan* p, const Sizes& z, int batch) {
 
 // ---- launches: items at most, and what they are shared out to.  grow (on the device) and the attention entry points go by the same numbers.
 struct Schedule {
-  int col_tiles, dec_items, pf_items;
+  int col_tiles, dec_items, pf_items, nw_items;
   int64_t dec_grid, pf_grid, pf_parts;      // items of a launch / of a split prefill launch, at most
+  int64_t nw_grid, nw_parts;                // items of few columns, and those of them that leave partial results, at most
 };
 Schedule schedule(const Sizes& z, int batch, int max_rows) {
   Schedule s;
   s.col_tiles = (z.G + 15) / 16;
   s.dec_items = std::max(1, page::kDecodeItems / (z.H_kv * s.col_tiles));
   s.dec_grid = s.dec_items + 2 * (int64_t)batch;
-  const int64_t cols = (int64_t)max_rows * z.G, most = cols / page::kQCols + std::min(batch, max_rows);
-  const bool split = max_rows > 0 && (cols + page::kQCols - 1) / page::kQCols * z.H_kv < page::kPfFill;
+  const int64_t cols = (int64_t)max_rows * z.G, seqs = std::min(batch, max_rows);
+  const int64_t most = cols > page::kNarrow ? cols / page::kQCols + std::min(seqs, cols / page::kNarrow) : 0;
+  const bool split = most > 0 && (cols + page::kQCols - 1) / page::kQCols * z.H_kv < page::kPfFill;
   s.pf_items = split ? std::max(1, page::kPfShares / z.H_kv) : 0;
   s.pf_parts = split ? s.pf_items + std::min<int64_t>(most, page::kPfFill / z.H_kv + 1) : 0;
   s.pf_grid = std::max(most, s.pf_parts);
+  // A block whose keys are split has more halves than a share: there are at most as many such blocks as shares' worth of work
+  s.nw_items = std::max(1, page::kNarrowItems / z.H_kv);
+  s.nw_grid = s.nw_items + std::min(seqs * ((page::kNarrow + page::kNCols - 1) / page::kNCols), cols / page::kNCols + seqs);
+  s.nw_parts = 2 * (int64_t)s.nw_items;
   return s;
 }
 
@@ -102,6 +108,8 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
 // Partials in the workspace: outputs, then (maximum, sum) pairs.
 size_t part_bytes(int64_t rows, int d) { return (size_t)rows * (d + 2) * 4; }
 
+int64_t prefill_rows(const Sizes& z, const Schedule& s) { return (s.pf_parts * page::kQCols + s.nw_parts * page::kNCols) * z.H_kv; }
+
 template <class F> int by_type(const Sizes& z, const page::AttnArgs& a, F f) {
   auto typed = [&](auto hd, auto mode) { return z.out_bf16 ? f(hd, mode, bf16_t{}) : f(hd, mode, float{}); };
   auto modal = [&](auto hd) {
@@ -121,7 +129,7 @@ size_t echokv_page_workspace_bytes(const echokv_shape* shape, int32_t batch, int
   Sizes z;
   if (check_shape(shape, &z) || batch <= 0 || batch > page::kMaxBatch || max_rows < 0 || (int64_t)max_rows * z.G >= (int64_t)1 << 30) return 0;
   const Schedule s = schedule(z, batch, max_rows);
-  const size_t dec = part_bytes(s.dec_grid * z.H_q, z.d), pf = part_bytes(s.pf_parts * z.H_kv * page::kQCols, z.d);
+  const size_t dec = part_bytes(s.dec_grid * z.H_q, z.d), pf = max_rows ? part_bytes(prefill_rows(z, s), z.d) : 0;
   return (std::max(dec, pf) + 255) / 256 * 256;
 }
 
@@ -138,8 +146,8 @@ int echokv_pages_grow(const echokv_shape* shape, const echokv_page_table* t, con
   a.len1 = seq_len_out; a.n_free1 = n_free_out; a.table = t->table; a.slot = row_slot; a.pos = row_pos;
   a.plan = {(int32_t*)plan->buf, t->batch};
   a.max_pages = t->max_pages; a.n_pages = t->n_pages; a.max_rows = plan->max_rows; a.H_q = z.H_q; a.H_kv = z.H_kv;
-  a.dec_items = s.dec_items; a.pf_items = s.pf_items;
-  a.rows_here = plan->max_rows <= 4096;
+  a.dec_items = s.dec_items; a.pf_items = s.pf_items; a.nw_items = s.nw_items;
+  a.rows_here = plan->max_rows <= 4096 && t->batch <= 1024;
   const hipStream_t st = (hipStream_t)hip_stream;
   if (t->batch <= 256 && plan->max_rows <= 1024) hipLaunchKernelGGL(page::grow_kernel<256>, dim3(1), dim3(256), 0, st, a);
   else hipLaunchKernelGGL(page::grow_kernel<1024>, dim3(1), dim3(1024), 0, st, a);
@@ -261,22 +269,28 @@ int echokv_page_prefill_attn(const echokv_shape* shape, const echokv_page_table*
   const Schedule s = schedule(z, t->batch, plan->max_rows);
   page::AttnArgs a;
   if ((rc = attn_args(z, t, c, plan, q, extras, out, lse_out, s, &a))) return rc;
-  const int64_t rows = s.pf_parts * z.H_kv * page::kQCols;
-  if (rows && (!workspace || !aligned16({workspace}) || workspace_bytes < part_bytes(rows, z.d))) return ECHOKV_ERR_WORKSPACE;
+  const int64_t rows = s.pf_parts * z.H_kv * page::kQCols, all = prefill_rows(z, s);
+  if (!workspace || !aligned16({workspace}) || workspace_bytes < part_bytes(all, z.d)) return ECHOKV_ERR_WORKSPACE;
   a.part_o = (float*)workspace;
-  a.part_ml = a.part_o + rows * z.d;
-  dim3 grid, merge;
-  if ((rc = launch_dims(s.pf_grid * z.H_kv, page::kPfThreads, &grid)) || (rc = launch_dims(s.pf_parts * z.H_kv, 256, &merge))) return rc;
-  merge.y = page::kQCols / 16;
+  a.nw_o = a.part_o + rows * z.d;
+  a.part_ml = a.part_o + all * z.d;
+  a.nw_ml = a.part_ml + rows * 2;
+  dim3 grid, narrow, merge;
+  if ((rc = launch_dims(s.pf_grid * z.H_kv, page::kPfThreads, &grid)) || (rc = launch_dims(s.nw_grid * z.H_kv, 256, &narrow)) ||
+      (rc = launch_dims((s.pf_parts + s.nw_parts) * z.H_kv, 256, &merge)))
+    return rc;
+  merge.y = page::kMergeParts;
   return by_type(z, a, [&](auto hd, auto mode, auto to) -> int {
-    constexpr int HD = decltype(hd)::value;
+    constexpr int HD = decltype(hd)::value, MODE = decltype(mode)::value;
     using TO = decltype(to);
-    hipLaunchKernelGGL((page::prefill_kernel<HD, decltype(mode)::value, TO>), grid, dim3(page::kPfThreads), 0, (hipStream_t)hip_stream, a);
-    LAUNCH_CHECK();
-    if (s.pf_parts) {
-      hipLaunchKernelGGL((page::prefill_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a);
+    if (s.pf_grid) {
+      hipLaunchKernelGGL((page::prefill_kernel<HD, MODE, TO>), grid, dim3(page::kPfThreads), 0, (hipStream_t)hip_stream, a);
       LAUNCH_CHECK();
     }
+    hipLaunchKernelGGL((page::narrow_kernel<HD, MODE, TO>), narrow, dim3(256), 0, (hipStream_t)hip_stream, a);
+    LAUNCH_CHECK();
+    hipLaunchKernelGGL((page::prefill_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a, (int)s.pf_parts);
+    LAUNCH_CHECK();
     return ECHOKV_OK;
   });
 }

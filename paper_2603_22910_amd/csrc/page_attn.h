@@ -8,6 +8,8 @@
 // products are cut off some 14 bits below the largest one (measured: up to 8e-5 of the sum of magnitudes, on average towards zero), where
 // those of bf16 products are good to 4e-8.
 #pragma once
+#include <type_traits>
+
 #include "page_kernels.h"
 
 namespace echokv {
@@ -29,6 +31,7 @@ struct AttnArgs {
   const float* slopes;
   void* out;
   float *lse, *part_o, *part_ml;        // partials: [item][H_q or H_kv * columns][d], then (maximum, sum) of each
+  float *nw_o, *nw_ml;                  // the same of prefill's items of few columns
   Plan plan;
   PlanKey key;
   float scale, cap;
@@ -103,10 +106,36 @@ template <typename TO> __device__ __forceinline__ void put4(TO* p, float4 v) {
   else *reinterpret_cast<float4*>(p) = v;
 }
 
+// Four dims of a finished row, and with the first four its log-sum-exp; a row that sees nothing: zeros and -inf.
+template <int HD, typename TO>
+__device__ __forceinline__ void finish(const AttnArgs& a, int64_t row, int d4, float4 acc, float M, float sum) {
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  put4(reinterpret_cast<TO*>(a.out) + row * HD + d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+  if (a.lse && d4 == 0) a.lse[row] = sum > 0.f ? (M + __log2f(sum)) * kLn2 : -INFINITY;
+}
+
+// Four dims of column c from the four waves' softmaxes of their own.
+template <int HD>
+__device__ __forceinline__ float4 join_waves(const float (&so)[4][16][HD + 4], const float (&sm)[4][16], const float (&sl)[4][16], int c, int d4,
+                                             float& M, float& sum) {
+  M = fmaxf(fmaxf(sm[0][c], sm[1][c]), fmaxf(sm[2][c], sm[3][c]));
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(sm[w][c] - M);
+    const float4 y = *reinterpret_cast<const float4*>(&so[w][c][d4]);
+    sum = fmaf(f, sl[w][c], sum);
+    acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y); acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
+  }
+  return acc;
+}
+
 // ---- decode: one token of every sequence.  A workgroup takes an item (a run of 64-token halves of a sequence's full pages, or its tail) of one KV
 // head and up to 16 of its query heads as columns.  Its four waves take the halves in turn, each with a softmax of its own; they are
 // joined in LDS.  What bounds it is the reading of the pages.
 constexpr int kDecodeItems = 1024;      // workgroups that the pages of a launch are shared out to
+constexpr int kNarrowItems = 1024;      // the same of a prefill launch's few-column part
 
 template <int HD, int MODE, typename TO>
 __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
@@ -250,22 +279,11 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
   __syncthreads();
   for (int x = tid; x < nc * (HD / 4); x += 256) {
     const int c = x / (HD / 4), d4 = x % (HD / 4) * 4;
-    const float M = fmaxf(fmaxf(sm[0][c], sm[1][c]), fmaxf(sm[2][c], sm[3][c]));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sm[w][c] - M);
-      const float4 y = *reinterpret_cast<const float4*>(&so[w][c][d4]);
-      sum = fmaf(f, sl[w][c], sum);
-      acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y); acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-    }
+    float M, sum;
+    const float4 acc = join_waves<HD>(so, sm, sl, c, d4, M, sum);
     const int h = kvh * a.G + ct * 16 + c;
     if (n_items == 1) {
-      const int64_t row = (int64_t)b * H_q + h;
-      const float inv = sum > 0.f ? 1.f / sum : 0.f;
-      put4(reinterpret_cast<TO*>(a.out) + row * HD + d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-      if (a.lse && d4 == 0) a.lse[row] = sum > 0.f ? (M + __log2f(sum)) * kLn2 : -INFINITY;
+      finish<HD, TO>(a, (int64_t)b * H_q + h, d4, acc, M, sum);
     } else {
       const int64_t row = (int64_t)item * H_q + h;
       *reinterpret_cast<float4*>(a.part_o + row * HD + d4) = acc;
@@ -276,7 +294,7 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
 
 // Joins `n` partials of one row, strided by `stride` rows, by a workgroup of 256 threads, in a fixed order.
 template <int HD, typename TO>
-__device__ __forceinline__ void join(const float* po, const float* pml, int n, int64_t stride, TO* out, float* lse) {
+__device__ __forceinline__ void join(const AttnArgs& a, const float* po, const float* pml, int n, int64_t stride, int64_t row) {
   constexpr int L = HD / 4, GR = 256 / L;
   __shared__ __attribute__((aligned(16))) float so[GR][HD];
   __shared__ float red[2][4];
@@ -308,9 +326,7 @@ __device__ __forceinline__ void join(const float* po, const float* pml, int n, i
       sum += ssum[k];
       acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    put4(out + d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-    if (lse && tid == 0) *lse = sum > 0.f ? (M + __log2f(sum)) * kLn2 : -INFINITY;
+    finish<HD, TO>(a, row, d4, acc, M, sum);
   }
 }
 
@@ -322,7 +338,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(AttnArgs a) {
   const int item0 = a.plan.dec()[b], n = a.plan.dec()[b + 1] - item0;
   if (n == 1) return;
   const int64_t row = (int64_t)b * H_q + h, first = (int64_t)item0 * H_q + h;
-  join<HD, TO>(a.part_o + first * HD, a.part_ml + first * 2, n, H_q, reinterpret_cast<TO*>(a.out) + row * HD, a.lse ? a.lse + row : nullptr);
+  join<HD, TO>(a, a.part_o + first * HD, a.part_ml + first * 2, n, H_q, row);
 }
 
 // ---- prefill: the queries of the new tokens.  A workgroup of eight waves takes 384 columns (query, query head of the KV head) of one sequence,
@@ -370,7 +386,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
   const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
   if (item >= n_items) return;
   const int B = a.key.batch, H_q = a.key.H_q, G = a.G;
-  const int b = find_item(a.plan.pf(), B, item), item0 = a.plan.pf()[b];
+  const int rank = find_item(a.plan.pf(), a.plan.w[kWideSeqs], item), item0 = a.plan.pf()[rank], b = __builtin_amdgcn_readfirstlane(a.plan.order()[rank]);
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
   const int chunk = a.plan.w[kPfChunk], shares = ((len + 63) / 64 - 1) / chunk + 1;
   const int cols = n * G;                   // (below 2^31: the host sees to it)
@@ -469,10 +485,12 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
   uint4 pf[CT][2];
   int page0 = page_of(h0), page1 = page_of(h0 + 1), page2 = page_of(h0 + 2);      // of this half and the next two
   bool have = false;                      // probabilities of the half before
-  // A step: products (values of the half before, keys of this one), barrier, softmax, barrier.  Waves 4 .. 7 run one barrier behind, so that of the two
-  // waves of a SIMD one has the matrix pipe while the other has the vector unit.
+  // A step: products (values of the half before, keys of this one) and softmax.  Waves 0 .. 3 meet the barrier behind the softmax, waves 4 .. 7, which share
+  // their SIMDs, behind the products: between two barriers the ones have the matrix pipe first and the others the vector unit.  The wave whose phase is the
+  // longer one goes first where both could issue (8192 queries, 32 heads: 515 us, without priorities 570, the other way round 564; with a cap 338, 358, 356).
+  const bool lag = wave >= 4;
   const auto step = [&](int hf) {
-    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_s_setprio(MODE == kCap ? 0 : 1);
     const auto stage = [&](int part) {
       if (part == 0) { place_k(hf + 1); fetch_k(hf + 2, page2); }
       if (part == 1) { place_v(hf); fetch_v(hf + 1, page1); }
@@ -497,8 +515,8 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
 #pragma unroll
         for (int c = 0; c < CT; ++c) s[c][n / KS] = mfma(f, qf[c][n % KS], n % KS ? s[c][n / KS] : floatx4_t{0.f, 0.f, 0.f, 0.f});
       });
-    barrier();
-    __builtin_amdgcn_s_setprio(0);
+    if (lag) barrier();
+    __builtin_amdgcn_s_setprio(MODE == kCap ? 1 : 0);
     kscale = exp_to_scale(scalar_byte(a.ke + head_of(page2)));
     vscale = exp_to_scale(scalar_byte(a.ve + head_of(page1)));
     const int next = scalar_word(pages + (max(min(hf + 3, full_halves - 1), 0) >> 1));
@@ -557,7 +575,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
     }
     page0 = page1; page1 = page2;
     page2 = hf + 3 < min(h1, full_halves) && (uint32_t)next < (uint32_t)a.n_pages ? next : -1;
-    barrier();
+    if (!lag) barrier();
   };
   if (h0 < h1) {
     fetch_k(h0, page0);
@@ -569,9 +587,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
     kscale = exp_to_scale(scalar_byte(a.ke + head_of(page1)));
     __builtin_amdgcn_s_waitcnt(0x0F70);                                 // vmcnt(0): no load of the queries is waited for inside the loop
     barrier();
-    if (wave >= 4) barrier();
     for (int hf = h0; hf <= h1; ++hf) step(hf);       // (the last step adds the last half's values and nothing else)
-    if (wave < 4) barrier();
   }
 
 #pragma unroll
@@ -596,40 +612,249 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
   }
 }
 
-// One workgroup per (item, KV head, 16 columns): joins the shares of the blocks whose first share the item is.
-template <int HD, typename TO>
-__global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a) {
-  constexpr int L = HD / 4, ROWS = 256 / L;
+// ---- prefill of few columns: a workgroup takes up to 32 columns of one sequence and KV head and a run of halves, which its four waves take in turn,
+// straight from memory to registers as in decode.  Waves that share halves instead of columns have work however few columns there are.
+template <int HD, int MODE, typename TO>
+__global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a) {
+  constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16, CT = kNCols / 16;
+  __shared__ __attribute__((aligned(16))) float so[4][16][HD + 4];
+  __shared__ float sm[4][16], sl[4][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   if (!made_for(a.plan, a.key)) return;
   const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
-  if (item >= a.plan.w[kPfItems]) return;
-  const int b = find_item(a.plan.pf(), a.key.batch, item), j = item - a.plan.pf()[b];
+  if (item >= a.plan.w[kNwItems]) return;
+  const int H_q = a.key.H_q, G = a.G, b = find_item(a.plan.nw(), a.key.batch, item), j = item - a.plan.nw()[b];
+  const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
+  const int chunk = a.plan.w[kNwChunk], halves = (len + 63) / 64, shares = (halves - 1) / chunk + 1, share = j % shares;
+  const int cols = n * G, x0 = j / shares * kNCols, nc = min(kNCols, cols - x0);
+  const int prefix = a.prefix ? min(max(a.prefix[b], 0), len) : 0;
+  const int full_halves = len / kTokens * 2, tail_rows = len % kTokens;
+  const int block_first = len0 + x0 / G, seen = max(len0 + (x0 + nc - 1) / G + 1, prefix);
+  const int begin = share * chunk, end = min(begin + chunk, (seen + 63) / 64);
+
+  uint4 qf[CT][KS];
+  int pos[CT];
+  float m[CT], l[CT], slope2[CT];
+  floatx4_t o[CT][U];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int x = x0 + min(16 * c + r, nc - 1), qi = x / G, head = kvh * G + x - qi * G;
+    pos[c] = len0 + qi;
+    const bf16_t* qp = a.q + ((int64_t)(row0 + qi) * H_q + head) * HD + 8 * g;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[c][s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
+    slope2[c] = MODE != kPlain && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    m[c] = kNoScore; l[c] = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) o[c][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const Mods md = mods_of(a);
+  const float fac = factor<MODE>(md);
+  const int32_t* pages = a.table + (int64_t)b * a.max_pages;
+  const int64_t D = (int64_t)a.key.H_kv * HD, tail = (int64_t)b * kTokens * D + kvh * HD;
+
+  const auto half = [&](int hf, auto paged) {
+    constexpr bool PAGE = decltype(paged)::value;
+    const int first = hf * 64;
+    uint4 vr[U];                          // values: codes of a full page
+    float vs = 0.f;
+    floatx4_t s[CT][4];
+    if constexpr (PAGE) {
+      const int page = scalar_word(pages + (hf >> 1));
+      if ((uint32_t)page >= (uint32_t)a.n_pages) return;
+      const int64_t ph = (int64_t)page * a.key.H_kv + kvh;
+      const uint4* kp = reinterpret_cast<const uint4*>(a.k + ph * (kTokens * HD) + (hf & 1) * (64 * HD)) + lane;
+      const uint4* vp = reinterpret_cast<const uint4*>(a.v + ph * (kTokens * HD) + (hf & 1) * (64 * HD)) + lane;
+      uint4 kr[4][KC];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) kr[t][c] = kp[(t * KC + c) * 64];
+#pragma unroll
+      for (int u = 0; u < U; ++u) vr[u] = vp[u * 64];
+      const float ks = exp_to_scale(scalar_byte(a.ke + ph));
+      vs = exp_to_scale(scalar_byte(a.ve + ph));
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          const uint4 f0 = widen8(kr[t][k].x, kr[t][k].y, ks), f1 = widen8(kr[t][k].z, kr[t][k].w, ks);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) {
+            s[c][t] = mfma(f0, qf[c][2 * k], k ? s[c][t] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+            s[c][t] = mfma(f1, qf[c][2 * k + 1], s[c][t]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);             // (a tile's codes are widened at a time)
+      }
+    } else {
+      const int t0 = first - full_halves * 64;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const uint32_t at32 = (uint32_t)min(t0 + 16 * t + r, tail_rows - 1) * (uint32_t)D + 8 * g;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const uint4 f = *reinterpret_cast<const uint4*>(a.kt + tail + (at32 + 32 * k));
+#pragma unroll
+          for (int c = 0; c < CT; ++c) s[c][t] = mfma(f, qf[c][k], k ? s[c][t] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    const bool masked = first + 63 > block_first && first + 63 >= prefix;
+    float v[CT][16], away[CT];
+    int at[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) at[i] = 16 * (i / 4) + i % 4;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[c][i] = s[c][i / 4][i % 4];
+      away[c] = (float)(first + 4 * g - pos[c]);
+    }
+    score<MODE>(v, md, slope2, away, at);
+    uint4 pf[CT][2];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      if (masked) {
+        const int lim = max(pos[c], prefix - 1) - first - 4 * g;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[c][i] = at[i] <= lim ? v[c][i] : -INFINITY;
+      }
+      float top = v[c][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, v[c][i]);
+      top = rows_max(top) * fac;
+      if (__any(top > m[c] + kRaise)) {
+        const float up = fmaxf(m[c], top), f = __builtin_amdgcn_exp2f(m[c] - up);
+        m[c] = up;
+        l[c] *= f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) o[c][u] *= f;
+      }
+      uint32_t p[8];
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(v[c][i], fac, -m[c])), p1 = __builtin_amdgcn_exp2f(fmaf(v[c][i + 1], fac, -m[c]));
+        l[c] += p0 + p1;
+        p[i / 2] = pack_bf16(p0, p1);        // (rounded once, as in the kernel for many columns)
+      }
+      pf[c][0] = make_uint4(p[0], p[1], p[2], p[3]); pf[c][1] = make_uint4(p[4], p[5], p[6], p[7]);
+    }
+    if constexpr (PAGE) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint4 v0 = widen8(vr[u].x, vr[u].y, vs), v1 = widen8(vr[u].z, vr[u].w, vs);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          o[c][u] = mfma(v0, pf[c][0], o[c][u]);
+          o[c][u] = mfma(v1, pf[c][1], o[c][u]);
+        }
+        if (u % 2) __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      const int t0 = first - full_halves * 64 + 4 * g;
+      const bf16_t* vp = a.vt + tail;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t at32[8];                 // (past the last row: that row again, with probabilities of zero)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) at32[x] = (uint32_t)min(t0 + 32 * k + 16 * (x / 4) + x % 4, tail_rows - 1) * (uint32_t)D + r;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          uint32_t w[4];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const uint32_t e = vp[at32[x] + 16 * u];
+            w[x / 2] = x % 2 ? w[x / 2] | e << 16 : e;
+          }
+          const uint4 f = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) o[c][u] = mfma(f, pf[c][k], o[c][u]);
+          if (u % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (32 loads at a time: more take more registers than there are)
+        }
+      }
+    }
+  };
+  int hf = begin + wave;
+  for (; hf < min(end, full_halves); hf += 4) half(hf, std::true_type{});
+  for (; hf < end; hf += 4) half(hf, std::false_type{});
+
+  const int slot = shares > 1 ? a.plan.nws()[b] + j : 0;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const float sum1 = rows_sum(l[c]);
+    __syncthreads();
+    if (g == 0) { sm[wave][r] = m[c]; sl[wave][r] = sum1; }
+#pragma unroll
+    for (int u = 0; u < U; ++u) *reinterpret_cast<floatx4_t*>(&so[wave][r][16 * u + 4 * g]) = o[c][u];
+    __syncthreads();
+    for (int x = tid; x < min(16, nc - 16 * c) * (HD / 4); x += 256) {
+      const int k = x / (HD / 4), d4 = x % (HD / 4) * 4;
+      float M, sum;
+      const float4 acc = join_waves<HD>(so, sm, sl, k, d4, M, sum);
+      if (shares == 1) {
+        const int col = x0 + 16 * c + k, qi = col / G;
+        const int64_t row = (int64_t)(row0 + qi) * H_q + kvh * G + (col - qi * G);
+        finish<HD, TO>(a, row, d4, acc, M, sum);
+      } else {
+        const int64_t part = ((int64_t)slot * a.key.H_kv + kvh) * kNCols + 16 * c + k;
+        *reinterpret_cast<float4*>(a.nw_o + part * HD + d4) = acc;
+        if (d4 == 0) *reinterpret_cast<float2*>(a.nw_ml + part * 2) = make_float2(M, sum);
+      }
+    }
+  }
+}
+
+// Joins the shares of split blocks: a wave per column, a workgroup per (item, KV head) and kMergeParts-th of its columns, where the item is its block's first
+// share.  Items of many columns first, then the slots of those of few.
+constexpr int kMergeParts = 8;
+template <int HD, typename TO>
+__global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a, int wide_items) {
+  constexpr int L = HD / 4, GR = 64 / L;               // lanes of a row, rows at a time
+  if (!made_for(a.plan, a.key)) return;
+  const int kvh = blockIdx.x % a.key.H_kv, at = blockIdx.x / a.key.H_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool narrow = at >= wide_items;
+  int b, j, chunk, bc, item;
+  if (narrow) {
+    item = at - wide_items;
+    if (item >= a.plan.w[kNwSlots]) return;
+    b = find_item(a.plan.nws(), a.key.batch, item); j = item - a.plan.nws()[b]; chunk = a.plan.w[kNwChunk]; bc = kNCols;
+  } else {
+    item = at;
+    if (item >= a.plan.w[kPfItems]) return;
+    const int rank = find_item(a.plan.pf(), a.plan.w[kWideSeqs], item);
+    b = __builtin_amdgcn_readfirstlane(a.plan.order()[rank]); j = item - a.plan.pf()[rank]; chunk = a.plan.w[kPfChunk]; bc = kQCols;
+  }
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b];
-  const int shares = ((len + 63) / 64 - 1) / a.plan.w[kPfChunk] + 1;
+  const int shares = ((len + 63) / 64 - 1) / chunk + 1;
   if (shares == 1 || j % shares) return;
-  const int cols = n * a.G;
-  const int x0 = ((cols - 1) / kQCols - j / shares) * kQCols;
-  const int d4 = threadIdx.x % L * 4;
-  for (int c = blockIdx.y * 16 + threadIdx.x / L; c < blockIdx.y * 16 + 16; c += ROWS) {
-    if (c >= cols - x0) break;
-    const int x = x0 + c;
-    const int64_t part = ((int64_t)item * a.key.H_kv + kvh) * kQCols + c, stride = (int64_t)a.key.H_kv * kQCols;
+  const int cols = n * a.G, x0 = (narrow ? j / shares : (cols - 1) / kQCols - j / shares) * bc;
+  const float* po = narrow ? a.nw_o : a.part_o;
+  const float* pml = narrow ? a.nw_ml : a.part_ml;
+  const int d4 = lane % L * 4, gr = lane / L;
+  for (int c = blockIdx.y * 4 + wave; c < bc && c < cols - x0; c += 4 * kMergeParts) {
+    const int64_t part = ((int64_t)item * a.key.H_kv + kvh) * bc + c, stride = (int64_t)a.key.H_kv * bc;
     float M = kNoScore;
-    for (int i = 0; i < shares; ++i) M = fmaxf(M, a.part_ml[(part + i * stride) * 2]);
+    for (int i = lane; i < shares; i += 64) M = fmaxf(M, pml[(part + i * stride) * 2]);
+    M = wave_max64(M);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
-    for (int i = 0; i < shares; ++i) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (part + i * stride) * 2);
-      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (part + i * stride) * HD + d4);
+#pragma unroll 4
+    for (int i = gr; i < shares; i += GR) {
+      const float2 ml = *reinterpret_cast<const float2*>(pml + (part + i * stride) * 2);
+      const float4 y = *reinterpret_cast<const float4*>(po + (part + i * stride) * HD + d4);
       const float f = __builtin_amdgcn_exp2f(ml.x - M);
       sum = fmaf(f, ml.y, sum);
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y); acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
     }
-    const int qi = x / a.G;
-    const int64_t row = (int64_t)(row0 + qi) * a.key.H_q + kvh * a.G + (x - qi * a.G);
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    put4(reinterpret_cast<TO*>(a.out) + row * HD + d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-    if (a.lse && d4 == 0) a.lse[row] = sum > 0.f ? (M + __log2f(sum)) * kLn2 : -INFINITY;
+#pragma unroll
+    for (int w = L; w < 64; w *= 2) {
+      sum += __shfl_xor(sum, w, 64);
+      acc.x += __shfl_xor(acc.x, w, 64); acc.y += __shfl_xor(acc.y, w, 64); acc.z += __shfl_xor(acc.z, w, 64); acc.w += __shfl_xor(acc.w, w, 64);
+    }
+    const int x = x0 + c, qi = x / a.G;
+    if (gr == 0) finish<HD, TO>(a, (int64_t)(row0 + qi) * a.key.H_q + kvh * a.G + (x - qi * a.G), d4, acc, M, sum);
   }
 }
 

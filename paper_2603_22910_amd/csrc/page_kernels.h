@@ -16,11 +16,14 @@ constexpr int kTokens = 128;            // of a page
 constexpr int kMaxBatch = 4096;         // sequences: their prefix sums fit LDS
 constexpr int kMinExp = -100;           // least exponent of a scale: products of two of them and of a query stay normal numbers
 constexpr int kQCols = 384;             // (query, query head) columns of a prefill workgroup
+constexpr int kNarrow = 192;            // a sequence of up to so many columns goes to the kernel for few of them
+constexpr int kNCols = 32;              // columns of its workgroups
 constexpr int kPfFill = 256;            // prefill workgroups that fill the chip, one to a compute unit: fewer are split over the keys
 
 // ---- plan: what grow leaves for the other kernels, int32 words.  Words 16 on: row_start, then the arrays below, each of batch + 1 words.
-enum { kStatus, kRows, kDecChunk, kDecItems, kPfChunk, kPfItems, kAppItems, kNewPages, kFree0, kBatch, kHq, kHkv, kMaxRows, kMagic, kHeadWords = 16 };
-constexpr int32_t kMagicWord = 0x45504731;
+enum { kStatus, kWideSeqs, kDecChunk, kDecItems, kPfChunk, kPfItems, kAppItems, kFree0, kBatch, kHq, kHkv, kMaxRows, kMagic, kNwChunk, kNwItems, kNwSlots, kHeadWords };
+static_assert(kHeadWords == 16, "row_start's place is documented");
+constexpr int32_t kMagicWord = 0x45504732;
 struct Plan {
   int32_t* w;
   int n;                                // batch
@@ -29,9 +32,12 @@ struct Plan {
   __host__ __device__ int32_t* len() const { return arr(1); }            // lengths with the new tokens
   __host__ __device__ int32_t* app() const { return arr(2); }            // prefix sums of append's items
   __host__ __device__ int32_t* dec() const { return arr(3); }            // ... of decode's items
-  __host__ __device__ int32_t* pf() const { return arr(4); }             // ... of prefill's items
-  __host__ __device__ int32_t* fresh() const { return arr(5); }          // ... of the new pages
-  static constexpr int kArrays = 6;
+  __host__ __device__ int32_t* fresh() const { return arr(4); }          // ... of the new pages
+  __host__ __device__ int32_t* pf() const { return arr(5); }             // ... of prefill's items of many columns, in the order of:
+  __host__ __device__ int32_t* order() const { return arr(6); }          // the sequences that have such, long ones first
+  __host__ __device__ int32_t* nw() const { return arr(7); }             // ... of its items of few columns
+  __host__ __device__ int32_t* nws() const { return arr(8); }            // ... of those that leave partial results
+  static constexpr int kArrays = 9;
 };
 
 // What the attention kernels make of a plan: sizes of the call that made it.
@@ -106,7 +112,7 @@ struct GrowArgs {
   int32_t *len1, *n_free1, *table, *slot, *pos;
   Plan plan;
   int max_pages, n_pages, max_rows, H_q, H_kv;
-  int dec_items, pf_items;              // items that share the work of a decode / prefill launch; pf_items = 0: blocks of queries suffice
+  int dec_items, pf_items, nw_items;    // items that share the work of a decode / prefill launch; pf_items = 0: blocks of queries suffice
   int rows_here;                        // the rows' slots are written by this launch, too
 };
 
@@ -125,120 +131,185 @@ __device__ __forceinline__ void grow_row(const GrowArgs& a, int row, int b, int 
 
 // Sums over the block's threads, in every thread.
 template <int N, int NT> __device__ __forceinline__ void block_sums(int64_t (&v)[N], int64_t (*lds)[NT / 64]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int W = NT / 64;
+  const int tid = threadIdx.x;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     for (int o = 32; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o, 64);
-    if (lane == 0) lds[i][wave] = v[i];
+    if ((tid & 63) == 0) lds[i][tid >> 6] = v[i];
+  }
+  __syncthreads();
+  static_assert(N * W <= NT && W <= 16, "a row of lanes per value");
+  if (tid < N * W) {
+    int64_t x = lds[tid / W][tid % W];
+    for (int o = W / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, W);
+    lds[tid / W][tid % W] = x;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = lds[i][0];
+  __syncthreads();
+}
+
+// Inclusive prefix sums over the block's threads, on top of carry, which takes the totals.
+template <int N, int NT> __device__ __forceinline__ void block_scan(int32_t (&v)[N], int32_t (&carry)[N], int32_t (*lds)[NT / 64]) {
+  constexpr int W = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(v[i], o, 64); if (lane >= o) v[i] += y; }
+    if (lane == 63) lds[i][wave] = v[i];
+  }
+  __syncthreads();
+  if (tid < N * W) {
+    int x = lds[tid / W][tid % W];
+    for (int o = 1; o < W; o <<= 1) { const int y = __shfl_up(x, o, W); if (tid % W >= o) x += y; }
+    lds[tid / W][tid % W] = x;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    int64_t s = 0;
-    for (int k = 0; k < NT / 64; ++k) s += lds[i][k];
-    v[i] = s;
+    v[i] += carry[i] + (wave ? lds[i][wave - 1] : 0);
+    carry[i] += lds[i][W - 1];
   }
   __syncthreads();
 }
 
+// Columns of a sequence with n new rows, and the blocks that a prefill kernel cuts them into.
+struct Cut { bool narrow; int blocks; };
+__device__ __forceinline__ Cut cut(int64_t n, int G) {
+  const int64_t cols = n * G;
+  const bool narrow = cols <= kNarrow;
+  return {narrow, (int)((cols + (narrow ? kNCols : kQCols) - 1) / (narrow ? kNCols : kQCols))};
+}
+
+// A length's place among 256, eight to a factor of two.
+__device__ __forceinline__ int bucket(int t) { return (int)(__float_as_uint((float)t) >> 20) - (127 << 3); }
+
 // All or nothing: lengths, sums and chunk sizes by one workgroup, a thread per sequence.
 template <int NT>
 __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
-  __shared__ int64_t red[6][NT / 64];
-  __shared__ int32_t wsum[5][NT / 64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = a.plan.n, G = a.H_q / a.H_kv;
+  constexpr int S = 8;
+  __shared__ int64_t red[S][NT / 64];
+  __shared__ int32_t wsum[6][NT / 64], hist[256];
+  __shared__ int32_t rows[NT + 1], lens[NT], fresh[NT];      // row_start, len, fresh, where the rows are looked at here
+  const int tid = threadIdx.x, B = a.plan.n, G = a.H_q / a.H_kv;
   const int64_t cap = (int64_t)a.max_pages * kTokens + kTokens - 1;
   const int n_free0 = *a.n_free0;
-  // rows, new pages, 64-token halves of full pages, query blocks, their halves; bits of what is wrong
-  int64_t s[6] = {0, 0, 0, 0, 0, 0};
-  uint32_t wrong = 0;
+  int first_l = 0, first_n = 0;                        // of sequence tid
+  if (tid < B) { first_l = a.len0[tid]; first_n = a.n_new[tid]; }
+  const auto len_of = [&](int b) { return b == tid ? first_l : a.len0[b]; };
+  const auto new_of = [&](int b) { return b == tid ? first_n : a.n_new[b]; };
+  // rows, new pages, 64-token halves of full pages; blocks of many columns and their halves, those of few; sequences of many; what is wrong
+  int64_t s[S] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int b = tid; b < B; b += NT) {
-    const int64_t l = a.len0[b], n = a.n_new[b];
-    if (l < 0 || l > cap || n < 0) { wrong |= 1; continue; }
-    if (l + n > cap) { wrong |= 2; continue; }
-    const int64_t t = l + n, qb = (n * G + kQCols - 1) / kQCols;
-    s[0] += n; s[1] += t / kTokens - l / kTokens; s[2] += t / kTokens * 2; s[3] += qb; s[4] += qb * ((t + 63) / 64);
+    const int64_t l = len_of(b), n = new_of(b);
+    if (l < 0 || l > cap || n < 0) { s[7] |= 1; continue; }
+    if (l + n > cap) { s[7] |= (int64_t)1 << 32; continue; }
+    const int64_t t = l + n;
+    const Cut c = cut(n, G);
+    s[0] += n; s[1] += t / kTokens - l / kTokens; s[2] += t / kTokens * 2;
+    if (c.narrow) s[5] += c.blocks * ((t + 63) / 64);
+    else { s[3] += c.blocks; s[4] += c.blocks * ((t + 63) / 64); s[6] += 1; }
   }
-  s[5] = (wrong & 1 ? 1 : 0) + (wrong & 2 ? (int64_t)1 << 32 : 0);
-  block_sums<6, NT>(s, red);
+  block_sums<S, NT>(s, red);
   int status = 0;
-  if ((s[5] & 0xffffffff) || n_free0 < 0 || n_free0 > a.n_pages) status |= 1;      // ECHOKV_PLAN_BAD_LENGTH
-  if (s[5] >> 32) status |= 2;                                                     // ECHOKV_PLAN_TABLE_FULL
+  if ((s[7] & 0xffffffff) || n_free0 < 0 || n_free0 > a.n_pages) status |= 1;      // ECHOKV_PLAN_BAD_LENGTH
+  if (s[7] >> 32) status |= 2;                                                     // ECHOKV_PLAN_TABLE_FULL
   if (!status && s[1] > n_free0) status |= 4;                                      // ECHOKV_PLAN_NO_PAGES
   if (!status && s[0] > a.max_rows) status |= 8;                                   // ECHOKV_PLAN_TOO_MANY_ROWS
   const bool ok = status == 0;
   if (!ok) {                                           // nobody grows: the halves of the lengths as they were
-    s[0] = s[1] = s[2] = s[3] = s[4] = 0;
     int64_t h[1] = {0};
-    for (int b = tid; b < B; b += NT) { const int64_t l = a.len0[b]; if (l >= 0 && l <= cap) h[0] += l / kTokens * 2; }
+    for (int b = tid; b < B; b += NT) { const int64_t l = len_of(b); if (l >= 0 && l <= cap) h[0] += l / kTokens * 2; }
     block_sums<1, NT>(h, red);
+    s[0] = s[1] = s[3] = s[4] = s[5] = s[6] = 0;
     s[2] = h[0];
   }
-  // decode: halves per item, four waves each a multiple of one half
-  const int dec_chunk = (int)max((int64_t)4, (s[2] + (int64_t)a.dec_items * 4 - 1) / ((int64_t)a.dec_items * 4) * 4);
+  // halves per item: of four waves each a multiple of one half (decode, few columns); of a share of the keys
+  const auto chunk4 = [](int64_t work, int items) { return (int)max((int64_t)4, (work + (int64_t)items * 4 - 1) / ((int64_t)items * 4) * 4); };
+  const int dec_chunk = chunk4(s[2], a.dec_items), nw_chunk = chunk4(s[5], a.nw_items);
   const int pf_chunk = a.pf_items && s[3] * a.H_kv < kPfFill ? (int)max((int64_t)8, (s[4] + a.pf_items - 1) / a.pf_items) : 0x7fffffff;
-  int32_t carry[5] = {0, 0, 0, 0, 0};
+  const int wide = (int)s[6], total = (int)s[0];
+  const auto wide_items = [&](int b) {                 // from the plan: the lengths may have been overwritten in place
+    const int n = a.plan.row_start()[b + 1] - (b ? a.plan.row_start()[b] : 0), t = a.plan.len()[b];
+    const Cut c = cut(n, G);
+    return c.narrow ? 0 : c.blocks * (((t + 63) / 64 - 1) / pf_chunk + 1);
+  };
+  int32_t carry[6] = {0, 0, 0, 0, 0, 0};
   for (int b0 = 0; b0 < B; b0 += NT) {
     const int b = b0 + tid;
     int l = 0, n = 0;
     if (b < B) {
-      const int64_t ll = a.len0[b];
+      const int64_t ll = len_of(b);
       l = ll >= 0 && ll <= cap ? (int)ll : 0;
-      n = ok ? a.n_new[b] : 0;
+      n = ok ? new_of(b) : 0;
+      a.len1[b] = ok ? l + n : (int)ll;
     }
-    const int t = l + n, f0 = l / kTokens, f1 = t / kTokens, halves = f1 * 2;
-    const int qb = (int)(((int64_t)n * G + kQCols - 1) / kQCols), seen = (t + 63) / 64;
-    int32_t v[5];
+    const int t = l + n, f0 = l / kTokens, f1 = t / kTokens, halves = f1 * 2, seen = (t + 63) / 64;
+    const Cut c = cut(n, G);
+    const int shares = n > 0 && c.narrow ? (seen - 1) / nw_chunk + 1 : 0;
+    int32_t v[6];
     v[0] = n;
     v[1] = n > 0 ? max(1, f1 - f0) : 0;
     v[2] = (halves + dec_chunk - 1) / dec_chunk + (t % kTokens ? 1 : 0);
-    v[3] = qb * (seen ? (seen - 1) / pf_chunk + 1 : 0);
-    v[4] = f1 - f0;
-    int32_t inc[5];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      int x = v[i];
-      for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o, 64); if (lane >= o) x += y; }
-      inc[i] = x;
-      if (lane == 63) wsum[i][wave] = x;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      int before = carry[i];
-      for (int k = 0; k < NT / 64; ++k) { const int y = wsum[i][k]; if (k < wave) before += y; carry[i] += y; }
-      inc[i] += before;
-    }
-    __syncthreads();
+    v[3] = f1 - f0;
+    v[4] = c.blocks * shares;
+    v[5] = shares > 1 ? c.blocks * shares : 0;
+    block_scan<6, NT>(v, carry, wsum);
     if (b < B) {
-      a.plan.row_start()[b + 1] = inc[0]; a.plan.app()[b + 1] = inc[1]; a.plan.dec()[b + 1] = inc[2];
-      a.plan.pf()[b + 1] = inc[3]; a.plan.fresh()[b + 1] = inc[4];
+      a.plan.row_start()[b + 1] = v[0]; a.plan.app()[b + 1] = v[1]; a.plan.dec()[b + 1] = v[2];
+      a.plan.fresh()[b + 1] = v[3]; a.plan.nw()[b + 1] = v[4]; a.plan.nws()[b + 1] = v[5];
       a.plan.len()[b] = t;
-      a.len1[b] = ok ? t : a.len0[b];
+      if (b0 == 0) { rows[tid + 1] = v[0]; lens[tid] = t; fresh[tid] = v[3] - (f1 - f0); }
+    }
+  }
+  int32_t items[1] = {0};
+  if (wide) {                                          // the longest sequences' blocks first: a long one that starts last would run on alone
+    for (int i = tid; i < 256; i += NT) hist[i] = 0;
+    __syncthreads();
+    for (int b = tid; b < B; b += NT) if (wide_items(b)) atomicAdd(&hist[bucket(a.plan.len()[b])], 1);
+    __syncthreads();
+    if (tid < 64) {                                    // places of the buckets, from the last one down
+      int x[4], sum = 0;
+      for (int i = 0; i < 4; ++i) { x[i] = sum; sum += hist[255 - 4 * tid - i]; }
+      int before = sum;
+      for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(before, o, 64); if (tid >= o) before += y; }
+      for (int i = 0; i < 4; ++i) hist[255 - 4 * tid - i] = before - sum + x[i];
+    }
+    __syncthreads();
+    // (which of two of a bucket comes first is a matter of chance, and of none to any result)
+    for (int b = tid; b < B; b += NT) if (wide_items(b)) a.plan.order()[atomicAdd(&hist[bucket(a.plan.len()[b])], 1)] = b;
+    __syncthreads();
+    for (int r0 = 0; r0 < wide; r0 += NT) {
+      const int r = r0 + tid;
+      int32_t w[1] = {0};
+      if (r < wide) { const int b = a.plan.order()[r]; w[0] = wide_items(b); }
+      block_scan<1, NT>(w, items, wsum);
+      if (r < wide) a.plan.pf()[r + 1] = w[0];
     }
   }
   if (tid == 0) {
     int32_t* w = a.plan.w;
-    for (int i : {0, 2, 3, 4, 5}) a.plan.arr(i)[0] = 0;
-    w[kStatus] = status; w[kRows] = (int)s[0]; w[kDecChunk] = dec_chunk; w[kDecItems] = carry[2]; w[kPfChunk] = pf_chunk; w[kPfItems] = carry[3];
-    w[kAppItems] = carry[1]; w[kNewPages] = carry[4]; w[kFree0] = n_free0;
+    for (int i : {0, 2, 3, 4, 5, 7, 8}) a.plan.arr(i)[0] = 0;
+    w[kStatus] = status; w[kWideSeqs] = wide; w[kDecChunk] = dec_chunk; w[kDecItems] = carry[2]; w[kPfChunk] = pf_chunk; w[kPfItems] = items[0];
+    w[kAppItems] = carry[1]; w[kFree0] = n_free0; w[kNwChunk] = nw_chunk; w[kNwItems] = carry[4]; w[kNwSlots] = carry[5];
     w[kBatch] = B; w[kHq] = a.H_q; w[kHkv] = a.H_kv; w[kMaxRows] = a.max_rows; w[kMagic] = kMagicWord;
     *a.n_free1 = n_free0 - (ok ? (int)s[1] : 0);
+    rows[0] = 0;
   }
   if (!a.rows_here) return;
-  __syncthreads();                                     // (the plan's arrays: written by this workgroup, read by it)
-  __threadfence_block();
-  for (int row = tid; row < (int)s[0]; row += NT) {
-    const int b = find_seq(a.plan.row_start(), B, row);
-    const int r0 = a.plan.row_start()[b];
-    grow_row(a, row, b, r0, a.plan.len()[b], a.plan.row_start()[b + 1] - r0, a.plan.fresh()[b], n_free0);
+  __syncthreads();
+  for (int row = tid; row < total; row += NT) {
+    const int b = find_seq(rows, B, row);
+    grow_row(a, row, b, rows[b], lens[b], rows[b + 1] - rows[b], fresh[b], n_free0);
   }
 }
 
 __global__ __launch_bounds__(256) void grow_rows_kernel(GrowArgs a) {
   const int row = blockIdx.x * 256 + threadIdx.x;
-  if (row >= a.plan.w[kRows]) return;
   const int32_t* rs = a.plan.row_start();
+  if (row >= rs[a.plan.n]) return;
   const int b = find_seq(rs, a.plan.n, row);
   grow_row(a, row, b, rs[b], a.plan.len()[b], rs[b + 1] - rs[b], a.plan.fresh()[b], a.plan.w[kFree0]);
 }

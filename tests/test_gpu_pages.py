@@ -374,6 +374,35 @@ def test_pages_past_4_gb():
     assert all(torch.equal(g.double().cpu(), h.flatten(1)) for g, h in zip(got, b.held(0)))
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_prefill_of_many_sequences_of_all_lengths(in_place):
+    """More sequences than the step's workgroup has threads; few and many columns, with and without split keys; outputs equal whether the lengths
+    are written in place or elsewhere."""
+    rng = np.random.default_rng(4)
+    batch = 1300
+    new = np.where(rng.random(batch) < 0.9, rng.integers(0, 3, batch), rng.integers(50, 140, batch)).tolist()
+    b = Batch((8, 2, 64), batch, max_pages=12, n_pages=2600)
+    b.grow(rng.integers(0, 300, batch).tolist())
+    before = b.table.seq_len.clone()
+    b.grow(new)
+    if not in_place:
+        n_new, len1, n_free = i32(new), b.table.seq_len.clone(), b.table.n_free.clone()
+        taken = sum(int(x) for x in (len1 // 128 - before // 128).tolist())
+        b.table.seq_len = before
+        b.table.n_free = n_free + taken                        # the same step from the same state: the same pages again
+        table = b.table.table.clone()
+        ek.pages_grow(b.shape, b.table, n_new, b.plan, torch.empty_like(before), torch.empty_like(n_free))
+        assert torch.equal(table, b.table.table)
+    q = b.random(sum(new), b.hq, b.d)
+    out, lse = b.prefill(q)
+    at = 0
+    for i, n in enumerate(new):
+        if n and (n > 3 or i % 100 == 0):
+            total = len(b.rows[i][0])
+            b.check(out[at:at + n], lse[at:at + n], q[at:at + n], i, list(range(total - n, total)), P_ONE)
+        at += n
+
+
 # ---- together
 def test_a_captured_step_follows_its_sequences():
     """grow, append and decode in one graph, replayed over the end of a block, with eager work in between; a twin takes the steps eagerly."""
