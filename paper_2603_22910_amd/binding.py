@@ -17,6 +17,7 @@ import numpy as np
 _LIB = None
 _call = None             # _hostcall.call or call_by_ctypes, and the addresses it is given, set by load()
 _APPEND = _WINDOW_APPEND = _DECODE = _DECODE_EX = 0
+_DTYPES = {}             # torch's dtypes by name
 _PAGE = {}               # the paged cache's entry points: name -> address
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libechokv.so")
 
@@ -209,6 +210,7 @@ def load() -> C.CDLL:
     address = lambda f: C.cast(f, C.c_void_p).value
     _APPEND, _WINDOW_APPEND = address(lib.echokv_cache_append), address(lib.echokv_window_append)
     _DECODE, _DECODE_EX = address(lib.echokv_decode_attn), address(lib.echokv_decode_attn_ex)
+    _DTYPES.update((n, getattr(torch, n)) for n in ("uint8", "int32", "bfloat16", "float32"))
     _PAGE.update((n, address(getattr(lib, "echokv_" + n))) for n in (
         "pages_grow", "pages_slots", "pages_release", "page_append", "page_read", "page_decode_attn", "page_prefill_attn"))
     _call = call
@@ -456,26 +458,51 @@ def augment_weights(shape: Shape, w_k, w_v, w_k_aug, w_v_aug, stream=None):
 # ---- paged 8-bit cache
 def _rows(t, dtype: str, least: int, what: str):
     """Address of a tensor argument: contiguous, of the named torch dtype, at least so many elements.  An address passes as it is."""
-    if t is None or isinstance(t, int):
+    if t is None or type(t) is int:
         return t
-    if not hasattr(t, "is_contiguous"):
+    try:
+        if t.is_contiguous() and t.dtype is _DTYPES[dtype] and t.is_cuda and t.numel() >= least:
+            return t.data_ptr()
+    except AttributeError:
         return _ptr(t)
-    if str(t.dtype) != "torch." + dtype:
+    if t.dtype is not _DTYPES[dtype]:
         raise TypeError(f"{what}: expected {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: not contiguous")
     if not t.is_cuda:
         raise ValueError(f"{what}: not on a GPU")
-    if t.numel() < least:
-        raise ValueError(f"{what}: {t.numel()} elements where {least} are needed")
-    return t.data_ptr()
+    raise ValueError(f"{what}: {t.numel()} elements where {least} are needed")
 
 
-class PageTable:
+class _Viewed:
+    """Tensors with a C view of them that is made once: a decode loop needs it in every call of every layer.  It is made again when an
+    attribute is set or a tensor's address has changed (its storage can be replaced)."""
+    _view = _at = None
+
+    def __setattr__(self, name, value):
+        self.__dict__[name] = value
+        self.__dict__["_view"] = None
+
+    def _viewed(self, at, make):
+        d = self.__dict__
+        if d["_view"] is None or at != self._at:
+            view = make()
+            d["_at"], d["_view"] = at, view
+        return d["_view"]
+
+
+class PageTable(_Viewed):
     """Block tables of a batch over a pool of pages: int32 tensors table [batch, max_pages], seq_len [batch], free_list [n_pages], n_free [1]."""
 
     def __init__(self, table, seq_len, free_list, n_free):
         self.table, self.seq_len, self.free_list, self.n_free = table, seq_len, free_list, n_free
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name == "table":
+            self.__dict__["batch"] = int(value.shape[0])
+        elif name == "free_list":
+            self.__dict__["n_pages"] = int(value.shape[0])
 
     @classmethod
     def empty(cls, batch: int, max_pages: int, n_pages: int, device="cuda") -> "PageTable":
@@ -485,22 +512,17 @@ class PageTable:
         return cls(torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32),
                    torch.arange(n_pages - 1, -1, -1, **i32), torch.full((1,), n_pages, **i32))
 
-    @property
-    def batch(self) -> int:
-        return int(self.table.shape[0])
-
-    @property
-    def n_pages(self) -> int:
-        return int(self.free_list.shape[0])
-
     def as_c(self) -> PageTableC:
+        return self._viewed((self.table.data_ptr(), self.seq_len.data_ptr(), self.free_list.data_ptr(), self.n_free.data_ptr()), self._make)
+
+    def _make(self) -> PageTableC:
         batch, max_pages = self.table.shape
-        return PageTableC(batch, max_pages, self.n_pages, _rows(self.table, "int32", 0, "table"),
-                          _rows(self.seq_len, "int32", batch, "seq_len"), _rows(self.free_list, "int32", 0, "free_list"),
+        return PageTableC(self.batch, max_pages, self.n_pages, _rows(self.table, "int32", self.batch * max_pages, "table"),
+                          _rows(self.seq_len, "int32", batch, "seq_len"), _rows(self.free_list, "int32", self.n_pages, "free_list"),
                           _rows(self.n_free, "int32", 1, "n_free"))
 
 
-class PageCache:
+class PageCache(_Viewed):
     """One layer's pages k, v (uint8 [n_pages, n_kv_heads, 128 * d]), scale bytes k_exp, v_exp (uint8 [n_pages, n_kv_heads]) and bf16 tails
     k_tail, v_tail [batch, 128, n_kv_heads * d]."""
 
@@ -516,6 +538,10 @@ class PageCache:
                    *[new(torch.bfloat16, batch, PAGE_TOKENS, h * d) for _ in range(2)])
 
     def as_c(self, shape: Shape, t: PageTable) -> PageCacheC:
+        return self._viewed((self.k.data_ptr(), self.v.data_ptr(), self.k_exp.data_ptr(), self.v_exp.data_ptr(), self.k_tail.data_ptr(),
+                             self.v_tail.data_ptr(), shape.n_kv_heads, shape.head_dim, t.n_pages, t.batch), lambda: self._make(shape, t))
+
+    def _make(self, shape: Shape, t: PageTable) -> PageCacheC:
         heads = t.n_pages * shape.n_kv_heads
         page, tail = heads * PAGE_TOKENS * shape.head_dim, t.batch * PAGE_TOKENS * shape.n_kv_heads * shape.head_dim
         return PageCacheC(_rows(self.k, "uint8", page, "k"), _rows(self.v, "uint8", page, "v"), _rows(self.k_exp, "uint8", heads, "k_exp"),
@@ -523,7 +549,7 @@ class PageCache:
                           _rows(self.v_tail, "bfloat16", tail, "v_tail"))
 
 
-class PagePlan:
+class PagePlan(_Viewed):
     """A step's plan: buf, a uint8 tensor of page_plan_bytes(batch) bytes, for up to max_rows new rows."""
 
     def __init__(self, buf, batch: int, max_rows: int):
@@ -548,8 +574,10 @@ class PagePlan:
         return self._words()[16:17 + self.batch]
 
     def as_c(self) -> PagePlanC:
-        return PagePlanC(_rows(self.buf, "uint8", 0, "plan"), self.buf.numel() if hasattr(self.buf, "numel") else page_plan_bytes(self.batch),
-                         self.max_rows)
+        return self._viewed(self.buf.data_ptr(), self._make)
+
+    def _make(self) -> PagePlanC:
+        return PagePlanC(_rows(self.buf, "uint8", 0, "plan"), self.buf.numel(), self.max_rows)
 
 
 def page_plan_bytes(batch: int) -> int:
@@ -599,7 +627,7 @@ _OUT = {BF16: "bfloat16", F32: "float32"}
 def page_read(shape: Shape, table: PageTable, cache: PageCache, row_slot, k_out, v_out, n_rows: Optional[int] = None, stream=None):
     load()
     n = int(row_slot.shape[0] if n_rows is None else n_rows)
-    least, dtype = n * shape.n_kv_heads * shape.head_dim, _OUT.get(shape.out_dtype, "")
+    least, dtype = n * shape.n_kv_heads * shape.head_dim, _OUT.get(shape.out_dtype, "float32")
     _check(_call(_PAGE["page_read"], _shape(shape), table.as_c(), cache.as_c(shape, table), _rows(row_slot, "int32", n, "row_slot"), n,
                  _rows(k_out, dtype, least, "k_out"), _rows(v_out, dtype, least, "v_out"), _stream(stream)), "echokv_page_read")
 
@@ -618,7 +646,7 @@ def page_decode_attn(shape: Shape, table: PageTable, cache: PageCache, plan: Pag
     rows = table.batch * shape.n_q_heads
     _check(_call(_PAGE["page_decode_attn"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(),
                  _rows(q, "bfloat16", rows * shape.head_dim, "q"), _score_extras(shape, table, softcap, slopes, None),
-                 _rows(out, _OUT.get(shape.out_dtype, ""), rows * shape.head_dim, "out"), _rows(lse_out, "float32", rows, "lse_out"),
+                 _rows(out, _OUT.get(shape.out_dtype, "float32"), rows * shape.head_dim, "out"), _rows(lse_out, "float32", rows, "lse_out"),
                  _ptr(workspace), nbytes, _stream(stream)), "echokv_page_decode_attn")
 
 
@@ -629,7 +657,7 @@ def page_prefill_attn(shape: Shape, table: PageTable, cache: PageCache, plan: Pa
     rows = plan.max_rows * shape.n_q_heads
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_call(_PAGE["page_prefill_attn"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(), _rows(q, "bfloat16", rows * shape.head_dim, "q"),
-                 _score_extras(shape, table, softcap, slopes, prefix_len), _rows(out, _OUT.get(shape.out_dtype, ""), rows * shape.head_dim, "out"),
+                 _score_extras(shape, table, softcap, slopes, prefix_len), _rows(out, _OUT.get(shape.out_dtype, "float32"), rows * shape.head_dim, "out"),
                  _rows(lse_out, "float32", rows, "lse_out"), _ptr(workspace), nbytes, _stream(stream)), "echokv_page_prefill_attn")
 
 
