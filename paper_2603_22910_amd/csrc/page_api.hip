@@ -275,21 +275,15 @@ int echokv_page_prefill_attn(const echokv_shape* shape, const echokv_page_table*
   a.nw_o = a.part_o + rows * z.d;
   a.part_ml = a.part_o + all * z.d;
   a.nw_ml = a.part_ml + rows * 2;
-  dim3 grid, narrow, merge;
-  if ((rc = launch_dims(s.pf_grid * z.H_kv, page::kPfThreads, &grid)) || (rc = launch_dims(s.nw_grid * z.H_kv, 256, &narrow)) ||
-      (rc = launch_dims((s.pf_parts + s.nw_parts) * z.H_kv, 256, &merge)))
-    return rc;
-  merge.y = page::kMergeParts;
+  dim3 grid;
+  const dim3 merge((unsigned)std::min<int64_t>((int64_t)plan->max_rows * z.H_q, page::kMergeBlocks));
+  if ((rc = launch_dims((s.pf_grid + s.nw_grid) * z.H_kv, page::kPfThreads, &grid))) return rc;
   return by_type(z, a, [&](auto hd, auto mode, auto to) -> int {
-    constexpr int HD = decltype(hd)::value, MODE = decltype(mode)::value;
+    constexpr int HD = decltype(hd)::value;
     using TO = decltype(to);
-    if (s.pf_grid) {
-      hipLaunchKernelGGL((page::prefill_kernel<HD, MODE, TO>), grid, dim3(page::kPfThreads), 0, (hipStream_t)hip_stream, a);
-      LAUNCH_CHECK();
-    }
-    hipLaunchKernelGGL((page::narrow_kernel<HD, MODE, TO>), narrow, dim3(256), 0, (hipStream_t)hip_stream, a);
+    hipLaunchKernelGGL((page::prefill_kernel<HD, decltype(mode)::value, TO>), grid, dim3(page::kPfThreads), 0, (hipStream_t)hip_stream, a, (int)s.pf_grid);
     LAUNCH_CHECK();
-    hipLaunchKernelGGL((page::prefill_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a, (int)s.pf_parts);
+    hipLaunchKernelGGL((page::prefill_merge_kernel<HD, TO>), merge, dim3(256), 0, (hipStream_t)hip_stream, a);
     LAUNCH_CHECK();
     return ECHOKV_OK;
   });

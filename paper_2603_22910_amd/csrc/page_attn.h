@@ -156,13 +156,13 @@ template <int HD, bool ONCE> struct Codes {
   }
 };
 
-// A wave's way through every fourth half of a sequence's pages.  Pages outside the pool are passed over: their tokens are seen by nobody.
-struct PageWalk {
+// A wave's way through every STEP-th half of a sequence's pages.  Pages outside the pool are passed over: their tokens are seen by nobody.
+template <int STEP> struct PageWalk {
   const int32_t* pages;
   int n_pages, end, H_kv, kvh;
   // The first half from hf on, and its (page, head).
   __device__ __forceinline__ bool find(int& hf, int64_t& ph) const {
-    for (; hf < end; hf += 4) {
+    for (; hf < end; hf += STEP) {
       const int page = scalar_word(pages + (hf >> 1));
       if ((uint32_t)page < (uint32_t)n_pages) { ph = (int64_t)page * H_kv + kvh; return true; }
     }
@@ -176,11 +176,8 @@ struct PageWalk {
 // ---- decode: one token of every sequence.  A workgroup takes an item (a run of 64-token halves of a sequence's full pages, or its tail) of one KV
 // head and up to 16 of its query heads as columns.  Its four waves take the halves in turn, each with a softmax of its own; they are
 // joined in LDS.  What bounds it is the reading of the pages.
-#ifndef NWI
-#define NWI 1024
-#endif
 constexpr int kDecodeItems = 1024;      // workgroups that the pages of a launch are shared out to
-constexpr int kNarrowItems = NWI;      // the same of a prefill launch's few-column part
+constexpr int kNarrowItems = 256;      // the same of a prefill launch's few-column part
 
 template <int HD, int MODE, typename TO>
 __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
@@ -212,7 +209,7 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
     // Codes of the next half are requested as soon as those of this one are used up: keys ahead of the softmax, values behind the second product.
     const int32_t* pages = a.table + (int64_t)b * a.max_pages;
     Codes<HD, true> x;
-    const PageWalk walk = {pages, a.n_pages, end, a.key.H_kv, kvh};
+    const PageWalk<4> walk = {pages, a.n_pages, end, a.key.H_kv, kvh};
     int64_t ph = 0;
     float ks = 0.f, vs = 0.f;
     int hf = begin + wave;
@@ -426,15 +423,13 @@ __device__ __forceinline__ void barrier() {
 }
 
 template <int HD, int MODE, typename TO>
-__global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
+__device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kvh, uint4* lds) {
   constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16, CT = kColTiles;
-  __shared__ __attribute__((aligned(16))) uint4 kbuf[2][4 * KS * 64], vbuf[2][2 * U * 64];      // halves as operands of 1 KB
+  const auto kbuf = [&](int hf) { return lds + (hf & 1) * (4 * KS * 64); };                   // halves as operands of 1 KB
+  const auto vbuf = [&](int hf) { return lds + (2 * 4 * KS + (hf & 1) * (2 * U)) * 64; };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-  if (!made_for(a.plan, a.key)) return;
-  const int n_items = a.plan.w[kPfItems];
-  const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
-  if (item >= n_items) return;
-  const int B = a.key.batch, H_q = a.key.H_q, G = a.G;
+  if (item >= a.plan.w[kPfItems]) return;
+  const int H_q = a.key.H_q, G = a.G;
   const int rank = find_item(a.plan.pf(), a.plan.w[kWideSeqs], item), item0 = a.plan.pf()[rank], b = __builtin_amdgcn_readfirstlane(a.plan.order()[rank]);
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
   const int chunk = a.plan.w[kPfChunk], shares = ((len + 63) / 64 - 1) / chunk + 1;
@@ -511,17 +506,17 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
         x0 = *reinterpret_cast<const uint4*>(p); x1 = *reinterpret_cast<const uint4*>(p + 32);
       }
     }
-    uint4* f = kbuf[(hf - h0) & 1] + (id & ~63) + id;      // operands 2 cf and 2 cf + 1 of 64 lanes
+    uint4* f = kbuf(hf - h0) + (id & ~63) + id;      // operands 2 cf and 2 cf + 1 of 64 lanes
     f[0] = x0; f[64] = x1;
   };
   const auto place_v = [&](int hf) {
     if (hf >= h1 || !has_v) return;
     if (hf < full_halves) {
-      uint4* f = vbuf[(hf - h0) & 1] + (vtid & ~63) + vtid;
+      uint4* f = vbuf(hf - h0) + (vtid & ~63) + vtid;
       f[0] = widen8(vraw.x, vraw.y, vscale); f[64] = widen8(vraw.z, vraw.w, vscale);
     } else {
       const int id = opaque(vtid), cl = id & 63, cf = id >> 6;
-      uint16_t* f = reinterpret_cast<uint16_t*>(vbuf[(hf - h0) & 1] + 2 * cf * 64 + cl);
+      uint16_t* f = reinterpret_cast<uint16_t*>(vbuf(hf - h0) + 2 * cf * 64 + cl);
       const int tok0 = (hf - full_halves) * 64 + 4 * (cl >> 4);
 #pragma unroll 1
       for (int y = 0; y < 16; ++y) {
@@ -545,7 +540,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
       if (part == 1) { place_v(hf); fetch_v(hf + 1, page1); }
     };
     if (have) {
-      with_operands<2 * U>(vbuf[(hf - 1 - h0) & 1] + lane, [&](int n, const uint4& f) {
+      with_operands<2 * U>(vbuf(hf - 1 - h0) + lane, [&](int n, const uint4& f) {
 #pragma unroll
         for (int c = 0; c < CT; ++c) o[c][n / 2] = mfma(f, pf[c][n % 2], o[c][n / 2]);
         if (n == 1) stage(0);                          // (in the shadow of the products)
@@ -560,7 +555,7 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
     have = hf < h1 && first < wave_seen && (hf >= full_halves || page0 >= 0);
     floatx4_t s[CT][4];
     if (have)
-      with_operands<4 * KS>(kbuf[(hf - h0) & 1] + lane, [&](int n, const uint4& f) {
+      with_operands<4 * KS>(kbuf(hf - h0) + lane, [&](int n, const uint4& f) {
 #pragma unroll
         for (int c = 0; c < CT; ++c) s[c][n / KS] = mfma(f, qf[c][n % KS], n % KS ? s[c][n / KS] : floatx4_t{0.f, 0.f, 0.f, 0.f});
       });
@@ -661,16 +656,15 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a) {
   }
 }
 
-// ---- prefill of few columns: a workgroup takes up to 32 columns of one sequence and KV head and a run of halves, which its four waves take in turn,
+// Few columns: a workgroup takes up to 32 columns of one sequence and KV head and a run of halves, which its eight waves take in turn,
 // straight from memory to registers as in decode.  Waves that share halves instead of columns have work however few columns there are.
 template <int HD, int MODE, typename TO>
-__global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a) {
+__device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh, uint4* lds) {
   constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16, CT = kNCols / 16;
-  __shared__ __attribute__((aligned(16))) float so[4][16][HD + 4];
-  __shared__ float sm[4][16], sl[4][16];
+  struct Join { float so[4][16][HD + 4], sm[4][16], sl[4][16]; };
+  static_assert(sizeof(Join) <= (2 * 4 * KS + 2 * 2 * U) * 1024, "in the other form's LDS");
+  Join& jn = *reinterpret_cast<Join*>(lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-  if (!made_for(a.plan, a.key)) return;
-  const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
   if (item >= a.plan.w[kNwItems]) return;
   const int H_q = a.key.H_q, G = a.G, b = find_item(a.plan.nw(), a.key.batch, item), j = item - a.plan.nw()[b];
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
@@ -703,7 +697,7 @@ __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a) {
   const int64_t D = (int64_t)a.key.H_kv * HD, tail = (int64_t)b * kTokens * D + kvh * HD;
 
   // Codes of the next half are requested as soon as those of this one are used up, as in decode; other blocks of the sequence read them, too.
-  const PageWalk walk = {pages, a.n_pages, min(end, full_halves), a.key.H_kv, kvh};
+  const PageWalk<kPfWaves> walk = {pages, a.n_pages, min(end, full_halves), a.key.H_kv, kvh};
   Codes<HD, false> codes;
   int64_t ph = 0;
   float ks = 0.f, vs = 0.f;
@@ -823,26 +817,39 @@ __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a) {
     walk.scales(a, ph, ks, vs);
   }
   while (hf < walk.end) {
-    int next = hf + 4;
+    int next = hf + kPfWaves;
     const bool more = walk.find(next, ph);
     half(hf, next, more, std::true_type{});
     hf = next;
   }
-  for (; hf < end; hf += 4) half(hf, 0, false, std::false_type{});
+  for (; hf < end; hf += kPfWaves) half(hf, 0, false, std::false_type{});
 
   const int slot = shares > 1 ? a.plan.nws()[b] + j : 0;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     const float sum1 = rows_sum(l[c]);
-    __syncthreads();
-    if (g == 0) { sm[wave][r] = m[c]; sl[wave][r] = sum1; }
+    const auto leave = [&] {
+      if (g == 0) { jn.sm[wave & 3][r] = m[c]; jn.sl[wave & 3][r] = l[c]; }
 #pragma unroll
-    for (int u = 0; u < U; ++u) *reinterpret_cast<floatx4_t*>(&so[wave][r][16 * u + 4 * g]) = o[c][u];
+      for (int u = 0; u < U; ++u) *reinterpret_cast<floatx4_t*>(&jn.so[wave & 3][r][16 * u + 4 * g]) = o[c][u];
+    };
+    l[c] = sum1;
     __syncthreads();
-    for (int x = tid; x < min(16, nc - 16 * c) * (HD / 4); x += 256) {
+    if (wave >= 4) leave();
+    __syncthreads();
+    if (wave < 4) {                                    // each of the first four waves takes one of the others in
+      const float m2 = jn.sm[wave][r], up = fmaxf(m[c], m2), f1 = __builtin_amdgcn_exp2f(m[c] - up), f2 = __builtin_amdgcn_exp2f(m2 - up);
+      l[c] = l[c] * f1 + jn.sl[wave][r] * f2;
+      m[c] = up;
+#pragma unroll
+      for (int u = 0; u < U; ++u) o[c][u] = o[c][u] * f1 + *reinterpret_cast<floatx4_t*>(&jn.so[wave][r][16 * u + 4 * g]) * f2;
+      leave();
+    }
+    __syncthreads();
+    for (int x = tid; x < min(16, nc - 16 * c) * (HD / 4); x += kPfThreads) {
       const int k = x / (HD / 4), d4 = x % (HD / 4) * 4;
       float M, sum;
-      const float4 acc = join_waves<HD>(so, sm, sl, k, d4, M, sum);
+      const float4 acc = join_waves<HD>(jn.so, jn.sm, jn.sl, k, d4, M, sum);
       if (shares == 1) {
         const int col = x0 + 16 * c + k, qi = col / G;
         const int64_t row = (int64_t)(row0 + qi) * H_q + kvh * G + (col - qi * G);
@@ -856,44 +863,49 @@ __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a) {
   }
 }
 
-// Joins the shares of split blocks: a wave per column, a workgroup per (item, KV head) and kMergeParts-th of its columns, where the item is its block's first
-// share.  Items of many columns first, then the slots of those of few.
-constexpr int kMergeParts = 8;
+template <int HD, int MODE, typename TO>
+__global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a, int wide_items) {
+  __shared__ __attribute__((aligned(16))) uint4 lds[(2 * 4 * (HD / 32) + 2 * 2 * (HD / 16)) * 64];
+  if (!made_for(a.plan, a.key)) return;
+  const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
+  if (item < wide_items) many_columns<HD, MODE, TO>(a, item, kvh, lds);
+  else few_columns<HD, MODE, TO>(a, item - wide_items, kvh, lds);
+}
+
+// Joins the shares of the columns whose keys are split: a wave per column and KV head, or where those are few a workgroup.
+constexpr int kMergeBlocks = 1024;
 template <int HD, typename TO>
-__global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a, int wide_items) {
+__global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a) {
   constexpr int L = HD / 4, GR = 64 / L;               // lanes of a row, rows at a time
   if (!made_for(a.plan, a.key)) return;
-  const int kvh = blockIdx.x % a.key.H_kv, at = blockIdx.x / a.key.H_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool narrow = at >= wide_items;
-  int b, j, chunk, bc, item;
-  if (narrow) {
-    item = at - wide_items;
-    if (item >= a.plan.w[kNwSlots]) return;
-    b = find_item(a.plan.nws(), a.key.batch, item); j = item - a.plan.nws()[b]; chunk = a.plan.w[kNwChunk]; bc = kNCols;
-  } else {
-    item = at;
-    if (item >= a.plan.w[kPfItems]) return;
-    const int rank = find_item(a.plan.pf(), a.plan.w[kWideSeqs], item);
-    b = __builtin_amdgcn_readfirstlane(a.plan.order()[rank]); j = item - a.plan.pf()[rank]; chunk = a.plan.w[kPfChunk]; bc = kQCols;
-  }
-  const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b];
-  const int shares = ((len + 63) / 64 - 1) / chunk + 1;
-  if (shares == 1 || j % shares) return;
-  const int cols = n * a.G, x0 = (narrow ? j / shares : (cols - 1) / kQCols - j / shares) * bc;
-  const float* po = narrow ? a.nw_o : a.part_o;
-  const float* pml = narrow ? a.nw_ml : a.part_ml;
-  const int d4 = lane % L * 4, gr = lane / L;
-  for (int c = blockIdx.y * 4 + wave; c < bc && c < cols - x0; c += 4 * kMergeParts) {
-    const int64_t part = ((int64_t)item * a.key.H_kv + kvh) * bc + c, stride = (int64_t)a.key.H_kv * bc;
+  const int B = a.key.batch, H_kv = a.key.H_kv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t units = (int64_t)a.plan.split()[B] * H_kv;
+  const bool whole = units <= kMergeBlocks;
+  for (int64_t i = whole ? blockIdx.x : blockIdx.x * 4 + wave; i < units; i += whole ? gridDim.x : gridDim.x * 4) {
+    const int kvh = (int)(i % H_kv), at = (int)(i / H_kv), b = find_item(a.plan.split(), B, at), x = at - a.plan.split()[b];
+    const int row0 = a.plan.row_start()[b], cols = a.plan.split()[b + 1] - a.plan.split()[b], halves = (a.plan.len()[b] + 63) / 64;
+    const bool narrow = cols <= kNarrow;
+    const int shares = (halves - 1) / a.plan.w[narrow ? kNwChunk : kPfChunk] + 1, bc = narrow ? kNCols : kQCols;
+    const int first = narrow ? a.plan.nws()[b] + x / bc * shares : a.plan.pf_of()[b] + ((cols - 1) / bc - x / bc) * shares;
+    const int64_t part = ((int64_t)first * H_kv + kvh) * bc + x % bc, stride = (int64_t)H_kv * bc;
+    const float* po = (narrow ? a.nw_o : a.part_o) + part * HD;
+    const float* pml = (narrow ? a.nw_ml : a.part_ml) + part * 2;
+    const int64_t row = (int64_t)(row0 + x / a.G) * a.key.H_q + kvh * a.G + x % a.G;
+    if (whole) {
+      join<HD, TO>(a, po, pml, shares, stride, row);
+      __syncthreads();
+      continue;
+    }
+    const int d4 = lane % L * 4, gr = lane / L;
     float M = kNoScore;
-    for (int i = lane; i < shares; i += 64) M = fmaxf(M, pml[(part + i * stride) * 2]);
+    for (int k = lane; k < shares; k += 64) M = fmaxf(M, pml[k * stride * 2]);
     M = wave_max64(M);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
 #pragma unroll 4
-    for (int i = gr; i < shares; i += GR) {
-      const float2 ml = *reinterpret_cast<const float2*>(pml + (part + i * stride) * 2);
-      const float4 y = *reinterpret_cast<const float4*>(po + (part + i * stride) * HD + d4);
+    for (int k = gr; k < shares; k += GR) {
+      const float2 ml = *reinterpret_cast<const float2*>(pml + k * stride * 2);
+      const float4 y = *reinterpret_cast<const float4*>(po + k * stride * HD + d4);
       const float f = __builtin_amdgcn_exp2f(ml.x - M);
       sum = fmaf(f, ml.y, sum);
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y); acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
@@ -903,8 +915,7 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a, int wide
       sum += __shfl_xor(sum, w, 64);
       acc.x += __shfl_xor(acc.x, w, 64); acc.y += __shfl_xor(acc.y, w, 64); acc.z += __shfl_xor(acc.z, w, 64); acc.w += __shfl_xor(acc.w, w, 64);
     }
-    const int x = x0 + c, qi = x / a.G;
-    if (gr == 0) finish<HD, TO>(a, (int64_t)(row0 + qi) * a.key.H_q + kvh * a.G + (x - qi * a.G), d4, acc, M, sum);
+    if (gr == 0) finish<HD, TO>(a, row, d4, acc, M, sum);
   }
 }
 

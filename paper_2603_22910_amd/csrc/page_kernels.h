@@ -37,7 +37,9 @@ struct Plan {
   __host__ __device__ int32_t* order() const { return arr(6); }          // the sequences that have such, long ones first
   __host__ __device__ int32_t* nw() const { return arr(7); }             // ... of its items of few columns
   __host__ __device__ int32_t* nws() const { return arr(8); }            // ... of those that leave partial results
-  static constexpr int kArrays = 9;
+  __host__ __device__ int32_t* split() const { return arr(9); }          // ... of the columns whose keys are split
+  __host__ __device__ int32_t* pf_of() const { return arr(10); }         // first of prefill's items of many columns, by sequence
+  static constexpr int kArrays = 11;
 };
 
 // What the attention kernels make of a plan: sizes of the call that made it.
@@ -191,7 +193,7 @@ template <int NT>
 __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
   constexpr int S = 8;
   __shared__ int64_t red[S][NT / 64];
-  __shared__ int32_t wsum[6][NT / 64], hist[256];
+  __shared__ int32_t wsum[7][NT / 64], hist[256];
   __shared__ int32_t rows[NT + 1], lens[NT], fresh[NT];      // row_start, len, fresh, where the rows are looked at here
   const int tid = threadIdx.x, B = a.plan.n, G = a.H_q / a.H_kv;
   const int64_t cap = (int64_t)a.max_pages * kTokens + kTokens - 1;
@@ -226,9 +228,31 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     s[0] = s[1] = s[3] = s[4] = s[5] = s[6] = 0;
     s[2] = h[0];
   }
-  // halves per item: of four waves each a multiple of one half (decode, few columns); of a share of the keys
-  const auto chunk4 = [](int64_t work, int items) { return (int)max((int64_t)4, (work + (int64_t)items * 4 - 1) / ((int64_t)items * 4) * 4); };
-  const int dec_chunk = chunk4(s[2], a.dec_items), nw_chunk = chunk4(s[5], a.nw_items);
+  // halves per item: as many for each of its waves (decode, few columns); of a share of the keys
+  const auto chunk = [](int64_t work, int items, int waves) { return (int)max((int64_t)waves, (work + (int64_t)items * waves - 1) / ((int64_t)items * waves) * waves); };
+  const int dec_chunk = chunk(s[2], a.dec_items, 4);
+  // Few columns: a block's last share is short, and one workgroup more than the chip holds at a time doubles the launch's time: of 1, 5/4, 6/4 and 7/4 times
+  // the even share, a wave each, the first that leaves no more items than that, else twice the even share.
+  int nw_chunk = chunk(s[5], a.nw_items, 8);
+  if (nw_chunk > 8) {
+    const int wave = tid >> 6, even = nw_chunk;
+    const auto candidate = [&](int k) { return (even * (4 + k) / 4 + 7) / 8 * 8; };
+    if (wave < 4) {
+      int64_t items = 0;
+      for (int b = tid & 63; b < B; b += 64) {
+        const int64_t n = a.n_new[b];
+        const Cut c = cut(n, G);
+        if (c.narrow && n) items += c.blocks * (((a.len0[b] + n + 63) / 64 - 1) / candidate(wave) + 1);
+      }
+      for (int o = 32; o > 0; o >>= 1) items += __shfl_xor(items, o, 64);
+      if ((tid & 63) == 0) red[0][wave] = items;
+    }
+    __syncthreads();
+    int k = 0;
+    while (k < 4 && red[0][k] > a.nw_items) ++k;
+    nw_chunk = candidate(k);
+    __syncthreads();
+  }
   const int pf_chunk = a.pf_items && s[3] * a.H_kv < kPfFill ? (int)max((int64_t)8, (s[4] + a.pf_items - 1) / a.pf_items) : 0x7fffffff;
   const int wide = (int)s[6], total = (int)s[0];
   const auto wide_items = [&](int b) {                 // from the plan: the lengths may have been overwritten in place
@@ -236,7 +260,7 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     const Cut c = cut(n, G);
     return c.narrow ? 0 : c.blocks * (((t + 63) / 64 - 1) / pf_chunk + 1);
   };
-  int32_t carry[6] = {0, 0, 0, 0, 0, 0};
+  int32_t carry[7] = {0, 0, 0, 0, 0, 0, 0};
   for (int b0 = 0; b0 < B; b0 += NT) {
     const int b = b0 + tid;
     int l = 0, n = 0;
@@ -248,18 +272,20 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     }
     const int t = l + n, f0 = l / kTokens, f1 = t / kTokens, halves = f1 * 2, seen = (t + 63) / 64;
     const Cut c = cut(n, G);
-    const int shares = n > 0 && c.narrow ? (seen - 1) / nw_chunk + 1 : 0;
-    int32_t v[6];
+    const int shares = n > 0 ? (seen - 1) / (c.narrow ? nw_chunk : pf_chunk) + 1 : 0, few = c.narrow ? c.blocks * shares : 0;
+    int32_t v[7];
     v[0] = n;
     v[1] = n > 0 ? max(1, f1 - f0) : 0;
     v[2] = (halves + dec_chunk - 1) / dec_chunk + (t % kTokens ? 1 : 0);
     v[3] = f1 - f0;
-    v[4] = c.blocks * shares;
-    v[5] = shares > 1 ? c.blocks * shares : 0;
-    block_scan<6, NT>(v, carry, wsum);
+    v[4] = few;
+    v[5] = shares > 1 ? few : 0;
+    v[6] = shares > 1 ? n * G : 0;
+    block_scan<7, NT>(v, carry, wsum);
     if (b < B) {
       a.plan.row_start()[b + 1] = v[0]; a.plan.app()[b + 1] = v[1]; a.plan.dec()[b + 1] = v[2];
       a.plan.fresh()[b + 1] = v[3]; a.plan.nw()[b + 1] = v[4]; a.plan.nws()[b + 1] = v[5];
+      a.plan.split()[b + 1] = v[6];
       a.plan.len()[b] = t;
       if (b0 == 0) { rows[tid + 1] = v[0]; lens[tid] = t; fresh[tid] = v[3] - (f1 - f0); }
     }
@@ -284,14 +310,15 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     for (int r0 = 0; r0 < wide; r0 += NT) {
       const int r = r0 + tid;
       int32_t w[1] = {0};
-      if (r < wide) { const int b = a.plan.order()[r]; w[0] = wide_items(b); }
+      int b = 0, mine = 0;
+      if (r < wide) { b = a.plan.order()[r]; w[0] = mine = wide_items(b); }
       block_scan<1, NT>(w, items, wsum);
-      if (r < wide) a.plan.pf()[r + 1] = w[0];
+      if (r < wide) { a.plan.pf()[r + 1] = w[0]; a.plan.pf_of()[b] = w[0] - mine; }
     }
   }
   if (tid == 0) {
     int32_t* w = a.plan.w;
-    for (int i : {0, 2, 3, 4, 5, 7, 8}) a.plan.arr(i)[0] = 0;
+    for (int i : {0, 2, 3, 4, 5, 7, 8, 9}) a.plan.arr(i)[0] = 0;
     w[kStatus] = status; w[kWideSeqs] = wide; w[kDecChunk] = dec_chunk; w[kDecItems] = carry[2]; w[kPfChunk] = pf_chunk; w[kPfItems] = items[0];
     w[kAppItems] = carry[1]; w[kFree0] = n_free0; w[kNwChunk] = nw_chunk; w[kNwItems] = carry[4]; w[kNwSlots] = carry[5];
     w[kBatch] = B; w[kHq] = a.H_q; w[kHkv] = a.H_kv; w[kMaxRows] = a.max_rows; w[kMagic] = kMagicWord;
