@@ -200,7 +200,7 @@ int echokv_page_append(const echokv_shape* shape, const echokv_page_table* t, co
   dim3 grid;
   // a sequence has an item for every block that is completed, at least one if it has new rows at all
   const int64_t items = plan->max_rows / page::kTokens + std::min(t->batch, plan->max_rows);
-  if ((rc = launch_dims(items * z.H_kv, 256, &grid))) return rc;
+  if ((rc = launch_dims(items * z.H_kv * 2, 256, &grid))) return rc;
   if (z.d == 64) hipLaunchKernelGGL(page::append_kernel<64>, grid, dim3(256), 0, (hipStream_t)hip_stream, a);
   else hipLaunchKernelGGL(page::append_kernel<128>, grid, dim3(256), 0, (hipStream_t)hip_stream, a);
   LAUNCH_CHECK();

@@ -131,12 +131,6 @@ __device__ __forceinline__ float4 join_waves(const float (&so)[4][16][HD + 4], c
   return acc;
 }
 
-// 16 bytes that are read once (non-temporal: 32 x 7808 tokens 98 -> 85.7 us, 5.2 -> 6.0 TB/s).
-__device__ __forceinline__ uint4 load_once(const uint4* p) {
-  typedef uint32_t v4_t __attribute__((ext_vector_type(4)));
-  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const v4_t*>(p)));
-}
-
 // The codes of a 64-token half of a page and KV head, as a lane takes them.
 template <int HD, bool ONCE> struct Codes {
   static constexpr int KC = HD / 64, U = HD / 16;

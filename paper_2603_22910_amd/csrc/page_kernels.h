@@ -100,9 +100,9 @@ __device__ __forceinline__ uint32_t finite_bits(uint32_t b) {        // b: 16 bi
   return m <= 0x7f60u ? b : m <= 0x7f80u ? (b & 0x8000u) | 0x7f60u : 0;
 }
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& odd) {
-  const uint32_t lo = w & 0xffffu, hi = w >> 16, a = finite_bits(lo), b = finite_bits(hi);
-  odd |= a != lo || b != hi;
-  return a | (b << 16);
+  const uint32_t x = finite_bits(w & 0xffffu) | (finite_bits(w >> 16) << 16);
+  odd |= x != w;
+  return x;
 }
 __device__ __forceinline__ uint4 finite8(uint4 x, bool& odd) {
   return make_uint4(finite_pair(x.x, odd), finite_pair(x.y, odd), finite_pair(x.z, odd), finite_pair(x.w, odd));
@@ -403,6 +403,18 @@ __global__ __launch_bounds__(NT) void release_kernel(ReleaseArgs a) {
   if (tid == 0) *a.n_free = n0 + (int)carry;
 }
 
+// Larger one of either half, as unsigned numbers: of magnitudes of bf16 numbers.
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+  typedef uint16_t pair_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(pair_t, a), __builtin_bit_cast(pair_t, b)));
+}
+
+__device__ __forceinline__ uint32_t magnitudes(uint4 x) {
+  return max_pair(max_pair(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), max_pair(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+}
+// Whether one of two magnitudes is one that finite_bits changes.
+__device__ __forceinline__ bool beyond(uint32_t m) { return (m & 0xffffu) > 0x7f60u || (m >> 16) > 0x7f60u; }
+
 // ---- rows into pages and tails
 struct StoreArgs {
   uint8_t *k, *v, *ke, *ve;
@@ -420,15 +432,31 @@ __device__ __forceinline__ int scale_byte(float amax) {
   return max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 127 + kMinExp);
 }
 
-// One workgroup per (item, KV head).  Item 0 of a sequence also moves the rows behind its last full block into the tail, after it has read
-// the tail's old rows for the first block.
+// Bytes b of four words (0 .. 3: one token or dim each) to four words of their own.
+__device__ __forceinline__ void transpose4(const uint32_t (&w)[4], uint32_t (&o)[4]) {
+  const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
+  const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+  o[0] = __builtin_amdgcn_perm(b0, a0, 0x05040100); o[1] = __builtin_amdgcn_perm(b0, a0, 0x07060302);
+  o[2] = __builtin_amdgcn_perm(b1, a1, 0x05040100); o[3] = __builtin_amdgcn_perm(b1, a1, 0x07060302);
+}
+
+// 16 bytes that are read once (non-temporal: 32 x 7808 tokens of decode 98 -> 85.7 us, 5.2 -> 6.0 TB/s).
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  typedef uint32_t v4_t __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const v4_t*>(p)));
+}
+
+// One workgroup per (item, KV head, side).  A block's rows are read once, into registers; its codes go through LDS into the page's order, 1 KB of
+// consecutive bytes per wave and store.  Item 0 of a sequence also moves the rows behind its last full block into the tail, after it has
+// read the tail's old rows for the first block.
 template <int HD>
-__global__ __launch_bounds__(256) void append_kernel(StoreArgs a) {
+__global__ __launch_bounds__(256, 4) void append_kernel(StoreArgs a) {
   constexpr int CPR = HD / 8, RPP = 256 / CPR, PASSES = kTokens / RPP;      // 16-byte chunks of a row, rows of a pass
-  __shared__ __attribute__((aligned(16))) uint8_t vbytes[kTokens * HD];
-  __shared__ float wmax[2][4];
+  constexpr int ROW = HD + 8;                          // bytes of a row in LDS: rows that are read together lie in banks of their own
+  __shared__ __attribute__((aligned(16))) uint8_t codes[kTokens * ROW];
+  __shared__ float wmax[4];
   const int tid = threadIdx.x, wave = tid >> 6;
-  const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
+  const int side = blockIdx.x & 1, kvh = (blockIdx.x >> 1) % a.key.H_kv, item = (blockIdx.x >> 1) / a.key.H_kv;
   if (!made_for(a.plan, a.key) || item >= a.plan.w[kAppItems]) return;
   const int b = find_item(a.plan.app(), a.key.batch, item), j = item - a.plan.app()[b];
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len1 = a.plan.len()[b], len0 = len1 - n;
@@ -436,90 +464,80 @@ __global__ __launch_bounds__(256) void append_kernel(StoreArgs a) {
   const int64_t D = (int64_t)a.key.H_kv * HD;
   const int rr = tid / CPR, cc = tid % CPR;
   bool odd = false;
-  const int64_t tail0 = (int64_t)b * kTokens * D + kvh * HD, new0 = (int64_t)row0 * D + kvh * HD;
+  bf16_t* tail = (side ? a.vt : a.kt) + (int64_t)b * kTokens * D + kvh * HD;
+  const bf16_t* rows = (side ? a.vn : a.kn) + (int64_t)row0 * D + kvh * HD;
   if (f1 > f0) {
     const int blk = f0 + j, page = a.table[(int64_t)b * a.max_pages + blk];
-    uint4 x[2][PASSES];
-    float m[2] = {0.f, 0.f};
+    uint4 x[PASSES];
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       const int tok = p * RPP + rr, at = blk * kTokens + tok;
-      const int64_t o = cc * 8 + (at < len0 ? tail0 + tok * D : new0 + (int64_t)(at - len0) * D);
-      x[0][p] = *reinterpret_cast<const uint4*>((at < len0 ? a.kt : a.kn) + o);
-      x[1][p] = *reinterpret_cast<const uint4*>((at < len0 ? a.vt : a.vn) + o);
+      const bf16_t* from = at < len0 ? tail : rows + (int64_t)(blk * kTokens - len0) * D;
+      x[p] = load_once(reinterpret_cast<const uint4*>(from + ((uint32_t)tok * (uint32_t)D + cc * 8)));
     }
+    uint32_t m = 0;                                    // two largest magnitudes' bits, of the even and the odd dims
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int p = 0; p < PASSES; ++p) m = max_pair(m, magnitudes(x[p]));
+    if (__any(beyond(m))) {                            // rare: not every row is looked at number by number
+      m = 0;
 #pragma unroll
-      for (int p = 0; p < PASSES; ++p) {
-        x[s][p] = finite8(x[s][p], odd);
-        float f[8];
-        unpack_bf16x8(x[s][p], f);
+      for (int p = 0; p < PASSES; ++p) { x[p] = finite8(x[p], odd); m = max_pair(m, magnitudes(x[p])); __builtin_amdgcn_sched_barrier(0); }
+    }
+    const float top = wave_max64(fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u)));
+    if ((tid & 63) == 0) wmax[wave] = top;
+    __syncthreads();
+    const int e = scale_byte(fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3])));
+    const float down = exp_to_scale(254 - e);          // 2^-e: e is within +-120
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m[s] = fmaxf(m[s], fabsf(f[i]));
-      }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      m[s] = wave_max64(m[s]);
-      if ((tid & 63) == 0) wmax[s][wave] = m[s];
+    for (int p = 0; p < PASSES; ++p) {
+      float f[8];
+      unpack_bf16x8(x[p], f);
+      uint2 c;
+      int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * down, f[1] * down, 0, false);
+      c.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * down, f[3] * down, w, true);
+      w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4] * down, f[5] * down, 0, false);
+      c.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6] * down, f[7] * down, w, true);
+      *reinterpret_cast<uint2*>(codes + (p * RPP + rr) * ROW + cc * 8) = c;
+      __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
-    int e[2];
+    if ((uint32_t)page < (uint32_t)a.n_pages) {
+      const int64_t ph = (int64_t)page * a.key.H_kv + kvh;
+      uint8_t* out = (side ? a.v : a.k) + ph * (kTokens * HD);
+      if (!side) {
+        for (int i = tid; i < kTokens * HD / 16; i += 256) {      // chunk of a lane (g, r), tile t and 64-dim part h
+          const int r = i & 15, g = (i >> 4) & 3, h = (i >> 6) % (HD / 64), t = (i >> 6) / (HD / 64);
+          const uint8_t* c = codes + (16 * t + r) * ROW + 64 * h + 8 * g;
+          const uint2 lo = *reinterpret_cast<const uint2*>(c), hi = *reinterpret_cast<const uint2*>(c + 32);
+          reinterpret_cast<uint4*>(out)[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
+      } else {
+        // a thread: four dims of 16 tokens (those of one lane group and half), four chunks whose bytes are the tokens'
+        for (int i = tid; i < HD / 4 * 8; i += 256) {
+          const int dq = i % (HD / 4), g = i / (HD / 4) % 4, h = i / (HD / 4) / 4;
+          uint32_t o[4][4];                            // [tile][dim]
 #pragma unroll
-    for (int s = 0; s < 2; ++s) e[s] = scale_byte(fmaxf(fmaxf(wmax[s][0], wmax[s][1]), fmaxf(wmax[s][2], wmax[s][3])));
-    const bool good = (uint32_t)page < (uint32_t)a.n_pages;
-    const int64_t ph = (int64_t)page * a.key.H_kv + kvh;
-    uint8_t* kp = a.k + ph * (kTokens * HD);
-    uint8_t* vp = a.v + ph * (kTokens * HD);
-    const float down[2] = {exp_to_scale(254 - e[0]), exp_to_scale(254 - e[1])};      // 2^-e: e is within +-120
+          for (int t = 0; t < 4; ++t) {
+            uint32_t w[4];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+            for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(codes + (h * 64 + t * 16 + g * 4 + k) * ROW + dq * 4);
+            transpose4(w, o[t]);
+          }
 #pragma unroll
-      for (int p = 0; p < PASSES; ++p) {
-        float f[8];
-        unpack_bf16x8(x[s][p], f);
-        uint2 c;
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * down[s], f[1] * down[s], 0, false);
-        c.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * down[s], f[3] * down[s], w, true);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4] * down[s], f[5] * down[s], 0, false);
-        c.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6] * down[s], f[7] * down[s], w, true);
-        const int tok = p * RPP + rr;
-        if (s == 0) {
-          if (good) *reinterpret_cast<uint2*>(kp + k_offset<HD>(tok, cc * 8)) = c;
-        } else {
-          *reinterpret_cast<uint2*>(vbytes + tok * HD + cc * 8) = c;
+          for (int d = 0; d < 4; ++d)
+            *reinterpret_cast<uint4*>(out + v_offset<HD>(h * 64 + g * 4, dq * 4 + d)) = make_uint4(o[0][d], o[1][d], o[2][d], o[3][d]);
         }
       }
-    __syncthreads();
-    if (good) {
-      // a thread: four dims of 16 tokens (those of one lane group and half), four chunks whose bytes are the tokens'
-      for (int i = tid; i < HD / 4 * 8; i += 256) {
-        const int dq = i % (HD / 4), g = i / (HD / 4) % 4, h = i / (HD / 4) / 4;
-        uint32_t o[4][4];                              // [dim][tile]
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          uint32_t w[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(vbytes + (h * 64 + t * 16 + g * 4 + k) * HD + dq * 4);
-          const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
-          const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
-          o[0][t] = __builtin_amdgcn_perm(b0, a0, 0x05040100); o[1][t] = __builtin_amdgcn_perm(b0, a0, 0x07060302);
-          o[2][t] = __builtin_amdgcn_perm(b1, a1, 0x05040100); o[3][t] = __builtin_amdgcn_perm(b1, a1, 0x07060302);
-        }
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-          *reinterpret_cast<uint4*>(vp + v_offset<HD>(h * 64 + g * 4, dq * 4 + d)) = make_uint4(o[d][0], o[d][1], o[d][2], o[d][3]);
-      }
-      if (tid == 0) { a.ke[ph] = (uint8_t)e[0]; a.ve[ph] = (uint8_t)e[1]; }
+      if (tid == 0) (side ? a.ve : a.ke)[ph] = (uint8_t)e;
     }
   }
   if (j == 0) {                                        // (its reads of the tail's old rows are behind the barriers above)
     const int first = f1 > f0 ? f1 * kTokens : len0;
     for (int i = tid; i < (len1 - first) * CPR; i += 256) {
       const int p = first + i / CPR;
-      const int64_t src = new0 + (int64_t)(p - len0) * D + i % CPR * 8, dst = tail0 + (int64_t)(p % kTokens) * D + i % CPR * 8;
-      *reinterpret_cast<uint4*>(a.kt + dst) = finite8(*reinterpret_cast<const uint4*>(a.kn + src), odd);
-      *reinterpret_cast<uint4*>(a.vt + dst) = finite8(*reinterpret_cast<const uint4*>(a.vn + src), odd);
+      uint4 x = load_once(reinterpret_cast<const uint4*>(rows + (int64_t)(p - len0) * D + i % CPR * 8));
+      if (beyond(magnitudes(x))) x = finite8(x, odd);
+      *reinterpret_cast<uint4*>(tail + (p % kTokens) * D + i % CPR * 8) = x;
     }
   }
   if (__any(odd) && (tid & 63) == 0) atomicOr(a.plan.w + kStatus, 16);            // ECHOKV_PLAN_NOT_FINITE
@@ -545,21 +563,26 @@ template <typename TO> __device__ __forceinline__ void put8(TO* p, uint4 b) {   
   }
 }
 
-// 128 rows of one KV head per workgroup.  A run of rows of one page goes through LDS, where the bytes of a value row lie 16 apart; shorter runs
-// than kLongRun rows, scattered rows and rows of tails are read where they are, all at once.
+template <typename TO> __device__ __forceinline__ void put4bf(TO* p, uint32_t a, uint32_t b) {      // four bf16 values
+  if constexpr (sizeof(TO) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(a, b);
+  else *reinterpret_cast<float4*>(p) = make_float4(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u));
+}
+
+// 128 rows of one KV head per workgroup.  Runs of at least kLongRun consecutive rows of a page are read in the page's order, 16 bytes a lane, and written
+// row by row; shorter ones, scattered rows and rows of tails are read where they are, all at once.
 constexpr int kLongRun = 16;
 template <int HD, typename TO>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs<TO> a) {
   constexpr int CPR = HD / 8, BYTES = kTokens * HD;
-  __shared__ __attribute__((aligned(16))) uint8_t kb[BYTES], vb[BYTES];
+  __shared__ __attribute__((aligned(16))) uint8_t kb[BYTES];
   __shared__ int32_t slots[kTokens];
   const int tid = threadIdx.x, lane = tid & 63, kvh = blockIdx.x % a.H_kv, row0 = blockIdx.x / a.H_kv * kTokens, n = min(kTokens, a.n_rows - row0);
   const int64_t D = (int64_t)a.H_kv * HD;
   if (tid < n) slots[tid] = a.slot[row0 + tid];
   __syncthreads();
-  // bit i: row i is of another page (or tail) than row i - 1; past the last row all bits are set
-  const auto differs = [&](int i) { return i >= n || i == 0 || (slots[i] >> 7) != (slots[i - 1] >> 7); };
-  const uint64_t edge[2] = {__ballot(differs(lane)), __ballot(differs(64 + lane))};
+  // bit i: row i does not follow row i - 1 in one page; past the last row all bits are set
+  const auto edge_at = [&](int i) { return i >= n || i == 0 || slots[i] < 0 || slots[i] != slots[i - 1] + 1 || (slots[i] & 127) == 0; };
+  const uint64_t edge[2] = {__ballot(edge_at(lane)), __ballot(edge_at(64 + lane))};
   const auto run_end = [&](int i) {                       // first edge behind row i
     const uint64_t lo = i < 63 ? edge[0] >> (i + 1) << (i + 1) : 0, hi = i < 64 ? edge[1] : i < 127 ? edge[1] >> (i - 63) << (i - 63) : 0;
     return lo ? __ffsll((long long)lo) - 1 : hi ? 63 + __ffsll((long long)hi) : kTokens;
@@ -567,16 +590,6 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs<TO> a) {
   const auto run_start = [&](int i) {                     // last edge up to row i
     const uint64_t hi = i < 64 ? 0 : edge[1] << (127 - i), lo = i < 64 ? edge[0] << (63 - i) : edge[0];
     return hi ? i - __clzll((long long)hi) : (i < 64 ? i : 63) - __clzll((long long)lo);
-  };
-  const auto put_page_row = [&](const uint8_t* kp, const uint8_t* vp, float ks, float vs, int tok, int c, int64_t o) {
-    const uint2 kk = *reinterpret_cast<const uint2*>(kp + k_offset<HD>(tok, c));
-    const uint8_t* vv = vp + v_offset<HD>(tok, c);
-    uint32_t w[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      w[h] = vv[64 * h] | (uint32_t)vv[64 * h + 16] << 8 | (uint32_t)vv[64 * h + 32] << 16 | (uint32_t)vv[64 * h + 48] << 24;
-    put8(a.ko + o, widen8(kk.x, kk.y, ks));
-    put8(a.vo + o, widen8(w[0], w[1], vs));
   };
   for (int x = tid; x < n * CPR; x += 256) {
     const int i = x / CPR, c = x % CPR * 8, s = slots[i];
@@ -588,26 +601,55 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs<TO> a) {
       put8(a.vo + o, *reinterpret_cast<const uint4*>(a.vt + t * D + kvh * HD + c));
     } else if ((s >> 7) < a.n_pages && run_end(i) - run_start(i) < kLongRun) {
       const int64_t ph = (int64_t)(s >> 7) * a.H_kv + kvh;
-      put_page_row(a.k + ph * BYTES, a.v + ph * BYTES, exp_to_scale(a.ke[ph]), exp_to_scale(a.ve[ph]), s & 127, c, o);
+      const uint2 kk = *reinterpret_cast<const uint2*>(a.k + ph * BYTES + k_offset<HD>(s & 127, c));
+      const uint8_t* vv = a.v + ph * BYTES + v_offset<HD>(s & 127, c);
+      uint32_t w[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        w[h] = vv[64 * h] | (uint32_t)vv[64 * h + 16] << 8 | (uint32_t)vv[64 * h + 32] << 16 | (uint32_t)vv[64 * h + 48] << 24;
+      put8(a.ko + o, widen8(kk.x, kk.y, exp_to_scale(a.ke[ph])));
+      put8(a.vo + o, widen8(w[0], w[1], exp_to_scale(a.ve[ph])));
     }
   }
-  for (int i = 0; i < n;) {
-    const int end = __builtin_amdgcn_readfirstlane(min(n, run_end(i))), first = slots[i], page = first >> 7;
-    if (first >= 0 && page < a.n_pages && end - i >= kLongRun) {
+  const auto long_run = [&](int i) { return i < n && edge_at(i) && slots[i] >= 0 && (slots[i] >> 7) < a.n_pages && min(n, run_end(i)) - i >= kLongRun; };
+  uint64_t starts[2] = {__ballot(long_run(lane)), __ballot(long_run(64 + lane))};
+#pragma unroll 1
+  for (int half = 0; half < 2; ++half)
+    for (uint64_t left = starts[half]; left; left &= left - 1) {
+      const int i = half * 64 + __ffsll((long long)left) - 1, end = __builtin_amdgcn_readfirstlane(min(n, run_end(i)));
+      const int first = __builtin_amdgcn_readfirstlane(slots[i]), page = first >> 7;
       const int64_t ph = (int64_t)page * a.H_kv + kvh;
-      const uint4* kp = reinterpret_cast<const uint4*>(a.k + ph * BYTES);
-      const uint4* vp = reinterpret_cast<const uint4*>(a.v + ph * BYTES);
       const float ks = exp_to_scale(a.ke[ph]), vs = exp_to_scale(a.ve[ph]);
-      __syncthreads();                                    // the page before is read
-      for (int x = tid; x < BYTES / 16; x += 256) { reinterpret_cast<uint4*>(kb)[x] = kp[x]; reinterpret_cast<uint4*>(vb)[x] = vp[x]; }
+      const int t0 = first & 127, count = end - i;
+      const int64_t out = (int64_t)(row0 + i - t0) * D + kvh * HD;      // of token 0 of the page
+      __syncthreads();                                    // the keys of the page before are read
+#pragma unroll
+      for (int x = 0; x < BYTES / 16; x += 256) reinterpret_cast<uint4*>(kb)[x + tid] = reinterpret_cast<const uint4*>(a.k + ph * BYTES)[x + tid];
       __syncthreads();
-      for (int x = tid; x < (end - i) * CPR; x += 256) {
-        const int row = i + x / CPR, c = x % CPR * 8;
-        put_page_row(kb, vb, ks, vs, slots[row] & 127, c, (row0 + row) * D + kvh * HD + c);
+#pragma unroll 4
+      for (int x = tid; x < count * CPR; x += 256) {
+        const int row = x / CPR, c = x % CPR * 8;
+        const uint2 kk = *reinterpret_cast<const uint2*>(kb + k_offset<HD>(t0 + row, c));
+        put8(a.ko + out + (int64_t)(t0 + row) * D + c, widen8(kk.x, kk.y, ks));
+      }
+      for (int x = tid; x < HD / 4 * 8; x += 256) {       // values: four dims of 16 tokens
+        const int dq = x % (HD / 4), g = x / (HD / 4) % 4, h = x / (HD / 4) / 4, tok = h * 64 + g * 4;
+        const uint4* p = reinterpret_cast<const uint4*>(a.v + ph * BYTES + v_offset<HD>(tok, dq * 4));
+        uint4 c[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) c[d] = p[d];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const auto word = [&](int d) { return t == 0 ? c[d].x : t == 1 ? c[d].y : t == 2 ? c[d].z : c[d].w; };
+          const uint32_t w[4] = {word(0), word(1), word(2), word(3)};
+          uint32_t o[4];
+          transpose4(w, o);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if ((uint32_t)(tok + 16 * t + k - t0) < (uint32_t)count) put4bf(a.vo + out + (tok + 16 * t + k) * D + dq * 4, widen<false>(o[k], vs), widen<true>(o[k], vs));
+        }
       }
     }
-    i = end;
-  }
 }
 
 }  // namespace page
