@@ -62,7 +62,8 @@ int check_plan(const echokv_page_plan* p, const Sizes& z, int batch) {
 // ---- launches: items at most, and what they are shared out to.  grow (on the device) and the attention entry points go by the same numbers.
 struct Schedule {
   int col_tiles, dec_items, pf_items, nw_items;
-  int64_t dec_grid, pf_grid, pf_parts;      // items of a launch / of a split prefill launch, at most
+  int64_t dec_grid, pf_grid;                // items of a launch, at most
+  int64_t pf_parts, pf_small;               // of a split prefill launch with large or small blocks
   int64_t nw_grid, nw_parts;                // items of few columns, and those of them that leave partial results, at most
 };
 Schedule schedule(const Sizes& z, int batch, int max_rows) {
@@ -71,11 +72,15 @@ Schedule schedule(const Sizes& z, int batch, int max_rows) {
   s.dec_items = std::max(1, page::kDecodeItems / (z.H_kv * s.col_tiles));
   s.dec_grid = s.dec_items + 2 * (int64_t)batch;
   const int64_t cols = (int64_t)max_rows * z.G, seqs = std::min(batch, max_rows);
-  const int64_t most = cols > page::kNarrow ? cols / page::kQCols + std::min(seqs, cols / page::kNarrow) : 0;
-  const bool split = most > 0 && (cols + page::kQCols - 1) / page::kQCols * z.H_kv < page::kPfFill;
-  s.pf_items = split ? std::max(1, page::kPfShares / z.H_kv) : 0;
-  s.pf_parts = split ? s.pf_items + std::min<int64_t>(most, page::kPfFill / z.H_kv + 1) : 0;
-  s.pf_grid = std::max(most, s.pf_parts);
+  // blocks of 384 columns, or of 128 if there are fewer than kPfMany workgroups of the large ones (so at most three times as many small ones)
+  const int64_t wide_seqs = cols > page::kNarrow ? std::min<int64_t>(seqs, cols / page::kNarrow) : 0, full = page::kPfFill / z.H_kv + 1;
+  const int64_t small = wide_seqs ? std::min<int64_t>(cols / page::kSCols + wide_seqs, 3 * (page::kPfMany / z.H_kv + 1)) : 0;
+  const int64_t large = wide_seqs ? cols / page::kQCols + wide_seqs : 0;
+  // split: fewer blocks than fill the chip, and no more shares than that beside each block's last one
+  s.pf_items = std::max(1, page::kPfFill / z.H_kv);
+  s.pf_parts = wide_seqs ? s.pf_items + std::min(large, full) : 0;
+  s.pf_small = wide_seqs ? s.pf_items + std::min(small, full) : 0;
+  s.pf_grid = std::max(std::max(large, small), std::max(s.pf_parts, s.pf_small));
   // A block whose keys are split has more halves than a share: there are at most as many such blocks as shares' worth of work
   s.nw_items = std::max(1, page::kNarrowItems / z.H_kv);
   s.nw_grid = s.nw_items + std::min(seqs * ((page::kNarrow + page::kNCols - 1) / page::kNCols), cols / page::kNCols + seqs);
@@ -101,6 +106,13 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
   a->plan = {(int32_t*)p->buf, t->batch};
   a->key = {t->batch, z.H_q, z.H_kv, p->max_rows};
   a->scale = z.scale; a->max_pages = t->max_pages; a->n_pages = t->n_pages; a->G = z.G; a->col_tiles = s.col_tiles;
+  if (x && x->softcap > 0.f) {
+    // cap2 tanh(to_arg x) as x times a polynomial in x^2, where its coefficients are numbers of fp32
+    const double k[4] = {0.99999997, -0.33332517, 0.13298439, -0.04913415}, arg = (double)z.scale / x->softcap;
+    a->to_arg = (float)arg;
+    if (arg > 1e-5 && arg < 1e4)
+      for (int i = 0; i < 4; ++i) a->tanh_k[i] = (float)(k[i] * std::pow(arg, 2 * i + 1) * x->softcap * page::kLog2e);
+  }
   if (x) { a->cap = x->softcap; a->slopes = x->slopes; a->prefix = x->prefix_len; }
   return ECHOKV_OK;
 }
@@ -108,12 +120,13 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
 // Partials in the workspace: outputs, then (maximum, sum) pairs.
 size_t part_bytes(int64_t rows, int d) { return (size_t)rows * (d + 2) * 4; }
 
-int64_t prefill_rows(const Sizes& z, const Schedule& s) { return (s.pf_parts * page::kQCols + s.nw_parts * page::kNCols) * z.H_kv; }
+int64_t wide_rows(const Sizes& z, const Schedule& s) { return std::max(s.pf_parts * page::kQCols, s.pf_small * page::kSCols) * z.H_kv; }
+int64_t prefill_rows(const Sizes& z, const Schedule& s) { return wide_rows(z, s) + s.nw_parts * page::kNCols * z.H_kv; }
 
 template <class F> int by_type(const Sizes& z, const page::AttnArgs& a, F f) {
   auto typed = [&](auto hd, auto mode) { return z.out_bf16 ? f(hd, mode, bf16_t{}) : f(hd, mode, float{}); };
   auto modal = [&](auto hd) {
-    if (a.cap > 0.f) return typed(hd, std::integral_constant<int, page::kCap>{});
+    if (a.cap > 0.f) return a.slopes ? typed(hd, std::integral_constant<int, page::kCapBias>{}) : typed(hd, std::integral_constant<int, page::kCap>{});
     return a.slopes ? typed(hd, std::integral_constant<int, page::kBias>{}) : typed(hd, std::integral_constant<int, page::kPlain>{});
   };
   return z.d == 64 ? modal(std::integral_constant<int, 64>{}) : modal(std::integral_constant<int, 128>{});
@@ -147,13 +160,14 @@ int echokv_pages_grow(const echokv_shape* shape, const echokv_page_table* t, con
   a.plan = {(int32_t*)plan->buf, t->batch};
   a.max_pages = t->max_pages; a.n_pages = t->n_pages; a.max_rows = plan->max_rows; a.H_q = z.H_q; a.H_kv = z.H_kv;
   a.dec_items = s.dec_items; a.pf_items = s.pf_items; a.nw_items = s.nw_items;
-  a.rows_here = plan->max_rows <= 4096 && t->batch <= 1024;
+  a.rows_here = plan->max_rows <= 4096 && t->batch <= 1024;      // (batch: what the workgroup below has threads for)
   const hipStream_t st = (hipStream_t)hip_stream;
   if (t->batch <= 256 && plan->max_rows <= 1024) hipLaunchKernelGGL(page::grow_kernel<256>, dim3(1), dim3(256), 0, st, a);
+  else if (t->batch <= 512) hipLaunchKernelGGL(page::grow_kernel<512>, dim3(1), dim3(512), 0, st, a);
   else hipLaunchKernelGGL(page::grow_kernel<1024>, dim3(1), dim3(1024), 0, st, a);
   LAUNCH_CHECK();
   if (!a.rows_here) {
-    hipLaunchKernelGGL(page::grow_rows_kernel, dim3((plan->max_rows + 255) / 256), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(page::grow_rows_kernel, dim3((plan->max_rows + page::kRowsPerBlock - 1) / page::kRowsPerBlock), dim3(page::kRowsPerBlock), 0, st, a);
     LAUNCH_CHECK();
   }
   return ECHOKV_OK;
@@ -269,7 +283,7 @@ int echokv_page_prefill_attn(const echokv_shape* shape, const echokv_page_table*
   const Schedule s = schedule(z, t->batch, plan->max_rows);
   page::AttnArgs a;
   if ((rc = attn_args(z, t, c, plan, q, extras, out, lse_out, s, &a))) return rc;
-  const int64_t rows = s.pf_parts * z.H_kv * page::kQCols, all = prefill_rows(z, s);
+  const int64_t rows = wide_rows(z, s), all = prefill_rows(z, s);
   if (!workspace || !aligned16({workspace}) || workspace_bytes < part_bytes(all, z.d)) return ECHOKV_ERR_WORKSPACE;
   a.part_o = (float*)workspace;
   a.nw_o = a.part_o + rows * z.d;

@@ -34,7 +34,7 @@ struct AttnArgs {
   float *nw_o, *nw_ml;                  // the same of prefill's items of few columns
   Plan plan;
   PlanKey key;
-  float scale, cap;
+  float scale, cap, to_arg, tanh_k[4];  // to_arg: scale / cap; tanh_k: see score
   int max_pages, n_pages, G, col_tiles, n_items;
 };
 
@@ -48,24 +48,48 @@ template <class F> __device__ __forceinline__ float across_rows(float v, F f) {
 __device__ __forceinline__ float rows_max(float v) { return across_rows(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float rows_sum(float v) { return across_rows(v, [](float a, float b) { return a + b; }); }
 
-// What is done to the raw products: nothing but a factor, which is left to the exponent's fused multiply-add; a bias; a cap, and maybe a bias.
-enum { kPlain, kBias, kCap };
-struct Mods { float scale2, cap2, to_arg; };
-template <int MODE> __device__ __forceinline__ float factor(const Mods& m) { return MODE == kPlain ? m.scale2 : 1.f; }
-__device__ __forceinline__ Mods mods_of(const AttnArgs& a) { return {a.scale * kLog2e, a.cap * kLog2e, a.cap > 0.f ? a.scale / a.cap : 0.f}; }
+// What is done to the raw products q.k: nothing but a factor, which is left to the exponent's fused multiply-add; a bias by distance, which the sums
+// start from; a cap; both, in which case the bias comes behind the cap.
+enum { kPlain, kBias, kCap, kCapBias };
+struct Mods { float scale2, cap2, to_arg, k0, k1, k2, k3; };
+template <int MODE> __device__ __forceinline__ float factor(const Mods& m) { return MODE == kPlain || MODE == kBias ? m.scale2 : 1.f; }
+__device__ __forceinline__ Mods mods_of(const AttnArgs& a) {
+  return {a.scale * kLog2e, a.cap * kLog2e, a.to_arg, a.tanh_k[0], a.tanh_k[1], a.tanh_k[2], a.tanh_k[3]};
+}
+// The slope of a column's head in the units in which it is added.
+template <int MODE> __device__ __forceinline__ float slope_of(const AttnArgs& a, int head) {
+  return MODE == kBias ? a.slopes[head] / a.scale : MODE == kCapBias ? a.slopes[head] * kLog2e : 0.f;
+}
+// What the products' sums of a column start from: away keys between the query and the lane's first key of the tile.
+template <int MODE> __device__ __forceinline__ floatx4_t start_of(float slope, float away) {
+  if constexpr (MODE != kBias) return floatx4_t{0.f, 0.f, 0.f, 0.f};
+  else return floatx4_t{slope * away, slope * (away + 1.f), slope * (away + 2.f), slope * (away + 3.f)};
+}
 
-// Raw products of C columns to scores in base 2.  c tanh(s / c): where all of a wave's arguments are small by the odd series, of which the terms past
-// x^9 are below 2^-25 of the first, else by (1 - e) / (1 + e), e = e^-2x, whose error is half a step of one, 2^-24 of the cap.
-// slope2[c]: slope in base 2; away[c]: key minus query position at the lane's first key, at[i] keys before the i-th.
+// Sums of C columns to scores (see factor).  c tanh(s / c), by the largest argument of the wave's: below 0.34 and 0.75 odd polynomials, tanh(x) / x in x^2
+// interpolated at the four or six Chebyshev nodes of the range, off by 3e-8 of the value at most; else (1 - e) / (1 + e), e = e^-2x, whose
+// error is half a step of one, 2^-24 of the cap.  The shortest has the scale and the cap in its coefficients (tanh_k) and takes five operations where the
+// last takes fourteen; the vector unit is what bounds prefill with a cap, and few scores come near one.
+// away[c]: key minus query position at the lane's first key, at[i] keys before the i-th.
 template <int MODE, int C, int N>
-__device__ __forceinline__ void score(float (&s)[C][N], const Mods& m, const float (&slope2)[C], const float (&away)[C], const int (&at)[N]) {
-  if constexpr (MODE == kCap) {
+__device__ __forceinline__ void score(float (&s)[C][N], const Mods& m, const float (&slope)[C], const float (&away)[C], const int (&at)[N]) {
+  if constexpr (MODE == kCap || MODE == kCapBias) {
     float top = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(s[c][i]));
-    if (__any(!(top * m.to_arg < 0.2f))) {
+    if (!__any(!(top * m.to_arg < 0.34f)) && m.k0 != 0.f) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float u = s[c][i] * s[c][i];
+          s[c][i] *= fmaf(u, fmaf(u, fmaf(u, m.k3, m.k2), m.k1), m.k0);
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (four at a time: more take more registers than there are)
+        }
+      }
+    } else if (__any(!(top * m.to_arg < 0.75f))) {
       const float arg2 = m.to_arg * (-2.f * kLog2e);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -73,29 +97,27 @@ __device__ __forceinline__ void score(float (&s)[C][N], const Mods& m, const flo
         for (int i = 0; i < N; ++i) {
           const float e = __builtin_amdgcn_exp2f(fabsf(s[c][i]) * arg2);        // (towards zero from either side: no overflow)
           s[c][i] = copysignf((m.cap2 - m.cap2 * e) * __builtin_amdgcn_rcpf(1.f + e), s[c][i]);
-          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (four at a time: more take more registers than there are)
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
       }
     } else {
+      constexpr float k[6] = {0.99999997f, -0.33332949f, 0.13325259f, -0.05333663f, 0.01956605f, -0.00470355f};
 #pragma unroll
       for (int c = 0; c < C; ++c) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const float x = s[c][i] * m.to_arg, x2 = x * x;
-          s[c][i] = x * m.cap2 * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+          const float x = s[c][i] * m.to_arg, u = x * x;
+          s[c][i] = x * m.cap2 * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, k[5], k[4]), k[3]), k[2]), k[1]), k[0]);
           if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
   }
-  if constexpr (MODE != kPlain) {
+  if constexpr (MODE == kCapBias) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float x = MODE == kCap ? s[c][i] : s[c][i] * m.scale2;
-        s[c][i] = fmaf(slope2[c], away[c] + (float)at[i], x);
-      }
+      for (int i = 0; i < N; ++i) s[c][i] = fmaf(slope[c], away[c] + (float)at[i], s[c][i]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -191,7 +213,7 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
 #pragma unroll
   for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
   const Mods md = mods_of(a);
-  const float fac = factor<MODE>(md), slope2[1] = {MODE != kPlain && a.slopes ? a.slopes[head] * kLog2e : 0.f};
+  const float fac = factor<MODE>(md), slope[1] = {slope_of<MODE>(a, head)};
 
   floatx4_t o[U];
 #pragma unroll
@@ -217,9 +239,10 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
       const bool more = walk.find(next, ph);
       float s1[1][16], (&s)[16] = s1[0];
       int step[16];
+      const float away = (float)(hf * 64 + 4 * g - (len - 1));
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        floatx4_t acc = {0.f, 0.f, 0.f, 0.f};
+        floatx4_t acc = start_of<MODE>(slope[0], away + (float)(16 * t));
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
           acc = mfma(widen8(x.k[t][c].x, x.k[t][c].y, ks), qf[2 * c], acc);
@@ -229,7 +252,7 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
         for (int i = 0; i < 4; ++i) { s[4 * t + i] = acc[i]; step[4 * t + i] = 16 * t + i; }
       }
       if (more) x.fetch_k(a, ph, next & 1, lane);
-      score<MODE>(s1, md, slope2, {(float)(hf * 64 + 4 * g - (len - 1))}, step);
+      score<MODE>(s1, md, slope, {away}, step);
       float top = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
@@ -268,17 +291,18 @@ __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
     if (t0 < rows) {
       const int64_t D = (int64_t)a.key.H_kv * HD, base = (int64_t)b * kTokens * D + kvh * HD;
       float s1[1][8], (&s)[8] = s1[0];
+      const float away = (float)(t0 + 4 * g - (rows - 1));
       int step[8];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const bf16_t* kp = a.kt + base + (int64_t)min(t0 + 16 * t + r, rows - 1) * D + 8 * g;
-        floatx4_t acc = {0.f, 0.f, 0.f, 0.f};
+        floatx4_t acc = start_of<MODE>(slope[0], away + (float)(16 * t));
 #pragma unroll
         for (int c = 0; c < KS; ++c) acc = mfma(*reinterpret_cast<const uint4*>(kp + 32 * c), qf[c], acc);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { s[4 * t + i] = acc[i]; step[4 * t + i] = 16 * t + i; }
       }
-      score<MODE>(s1, md, slope2, {(float)(t0 + 4 * g - (rows - 1))}, step);
+      score<MODE>(s1, md, slope, {away}, step);
       float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -385,8 +409,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(AttnArgs a) {
 // 48 to a wave, and walks the 64-token halves of the keys they see: codes to registers, widened to bf16 on their way into LDS
 // (once for all eight waves), operands back in the order of the lanes.  Two buffers, one barrier per half.  Where few blocks of queries face
 // long contexts the keys are split into shares, joined by a second launch.
-constexpr int kPfWaves = 8, kPfThreads = 64 * kPfWaves, kColTiles = kQCols / kPfWaves / 16;
-constexpr int kPfShares = 512;           // workgroups that too few blocks of queries are split into
+constexpr int kPfWaves = 8, kPfThreads = 64 * kPfWaves;
 constexpr float kRaise = 8.f;           // the reference of a softmax is raised once the maximum has passed it by 2^8: sums and outputs hold that
 
 // The same number, of which the compiler knows nothing: what depends on it stays where it is used (out of a loop's registers).
@@ -416,9 +439,9 @@ __device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
 }
 
-template <int HD, int MODE, typename TO>
+template <int HD, int MODE, typename TO, int CT>
 __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kvh, uint4* lds) {
-  constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16, CT = kColTiles;
+  constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16, QC = kPfWaves * 16 * CT;
   const auto kbuf = [&](int hf) { return lds + (hf & 1) * (4 * KS * 64); };                   // halves as operands of 1 KB
   const auto vbuf = [&](int hf) { return lds + (2 * 4 * KS + (hf & 1) * (2 * U)) * 64; };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
@@ -428,12 +451,12 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
   const int chunk = a.plan.w[kPfChunk], shares = ((len + 63) / 64 - 1) / chunk + 1;
   const int cols = n * G;                   // (below 2^31: the host sees to it)
-  const int blocks = (cols - 1) / kQCols + 1, j = item - item0, share = j % shares;
-  const int x0 = (blocks - 1 - j / shares) * kQCols;    // the longest ones first
+  const int blocks = (cols - 1) / QC + 1, j = item - item0, share = j % shares;
+  const int x0 = (blocks - 1 - j / shares) * QC;    // the longest ones first
   const int prefix = a.prefix ? min(max(a.prefix[b], 0), len) : 0;
   const int full_halves = len / kTokens * 2, tail_rows = len % kTokens;
   // what the block and the wave see: keys up to their last column's own, or the prefix
-  const int xl = min(x0, cols - kQCols) + kQCols - 1;
+  const int xl = min(x0, cols - QC) + QC - 1;
   const int seen = max(len0 + xl / G + 1, prefix);
   const int h0 = share * min(chunk, 0x3fffffff), h1 = min((seen + 63) / 64, shares > 1 ? h0 + chunk : 0x7fffffff);
   const int w0 = min(x0 + wave * (16 * CT), cols);      // (cols: none of the wave's columns exists)
@@ -443,7 +466,7 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
 
   uint4 qf[CT][KS];
   int pos[CT];
-  float m[CT], l[CT], slope2[CT];
+  float m[CT], l[CT], slope[CT];
   floatx4_t o[CT][U];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -453,7 +476,7 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
     const bf16_t* qp = a.q + ((int64_t)(row0 + qi) * H_q + head) * HD + 8 * g;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[c][s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
-    slope2[c] = MODE != kPlain && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    slope[c] = slope_of<MODE>(a, head);
     m[c] = kNoScore; l[c] = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) o[c][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
@@ -527,8 +550,9 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
   // their SIMDs, behind the products: between two barriers the ones have the matrix pipe first and the others the vector unit.  The wave whose phase is the
   // longer one goes first where both could issue (8192 queries, 32 heads: 515 us, without priorities 570, the other way round 564; with a cap 338, 358, 356).
   const bool lag = wave >= 4;
+  constexpr bool CAPPED = MODE == kCap || MODE == kCapBias;
   const auto step = [&](int hf) {
-    __builtin_amdgcn_s_setprio(MODE == kCap ? 0 : 1);
+    __builtin_amdgcn_s_setprio(CAPPED ? 0 : 1);
     const auto stage = [&](int part) {
       if (part == 0) { place_k(hf + 1); fetch_k(hf + 2, page2); }
       if (part == 1) { place_v(hf); fetch_v(hf + 1, page1); }
@@ -551,10 +575,10 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
     if (have)
       with_operands<4 * KS>(kbuf(hf - h0) + lane, [&](int n, const uint4& f) {
 #pragma unroll
-        for (int c = 0; c < CT; ++c) s[c][n / KS] = mfma(f, qf[c][n % KS], n % KS ? s[c][n / KS] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+        for (int c = 0; c < CT; ++c) s[c][n / KS] = mfma(f, qf[c][n % KS], n % KS ? s[c][n / KS] : start_of<MODE>(slope[c], (float)(first + 16 * (n / KS) + 4 * g - pos[c])));
       });
     if (lag) barrier();
-    __builtin_amdgcn_s_setprio(MODE == kCap ? 1 : 0);
+    __builtin_amdgcn_s_setprio(CAPPED ? 1 : 0);
     kscale = exp_to_scale(scalar_byte(a.ke + head_of(page2)));
     vscale = exp_to_scale(scalar_byte(a.ve + head_of(page1)));
     const int next = scalar_word(pages + (max(min(hf + 3, full_halves - 1), 0) >> 1));
@@ -571,7 +595,7 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
         for (int i = 0; i < 16; ++i) v[c][i] = s[c][i / 4][i % 4];
         away[c] = (float)(first + 4 * g - pos[c]);
       }
-      score<MODE>(v, md, slope2, away, at);
+      score<MODE>(v, md, slope, away, at);
       bool higher = false;
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
@@ -642,7 +666,7 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
         put4(reinterpret_cast<TO*>(a.out) + row * HD + 16 * u + 4 * g, make_float4(o[c][u][0] * inv, o[c][u][1] * inv, o[c][u][2] * inv, o[c][u][3] * inv));
       if (a.lse && g == 0) a.lse[row] = sum > 0.f ? (m[c] + __log2f(sum)) * kLn2 : -INFINITY;
     } else {
-      const int64_t part = ((int64_t)item * a.key.H_kv + kvh) * kQCols + (x - x0);
+      const int64_t part = ((int64_t)item * a.key.H_kv + kvh) * QC + (x - x0);
 #pragma unroll
       for (int u = 0; u < U; ++u) *reinterpret_cast<floatx4_t*>(a.part_o + part * HD + 16 * u + 4 * g) = o[c][u];
       if (g == 0) *reinterpret_cast<float2*>(a.part_ml + part * 2) = make_float2(m[c], sum);
@@ -671,7 +695,7 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
 
   uint4 qf[CT][KS];
   int pos[CT];
-  float m[CT], l[CT], slope2[CT];
+  float m[CT], l[CT], slope[CT];
   floatx4_t o[CT][U];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -680,7 +704,7 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
     const bf16_t* qp = a.q + ((int64_t)(row0 + qi) * H_q + head) * HD + 8 * g;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[c][s] = *reinterpret_cast<const uint4*>(qp + 32 * s);
-    slope2[c] = MODE != kPlain && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    slope[c] = slope_of<MODE>(a, head);
     m[c] = kNoScore; l[c] = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) o[c][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
@@ -707,7 +731,7 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
           const uint4 f0 = widen8(codes.k[t][k].x, codes.k[t][k].y, ks), f1 = widen8(codes.k[t][k].z, codes.k[t][k].w, ks);
 #pragma unroll
           for (int c = 0; c < CT; ++c) {
-            s[c][t] = mfma(f0, qf[c][2 * k], k ? s[c][t] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+            s[c][t] = mfma(f0, qf[c][2 * k], k ? s[c][t] : start_of<MODE>(slope[c], (float)(first + 16 * t + 4 * g - pos[c])));
             s[c][t] = mfma(f1, qf[c][2 * k + 1], s[c][t]);
           }
         }
@@ -723,7 +747,7 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
         for (int k = 0; k < KS; ++k) {
           const uint4 f = *reinterpret_cast<const uint4*>(a.kt + tail + (at32 + 32 * k));
 #pragma unroll
-          for (int c = 0; c < CT; ++c) s[c][t] = mfma(f, qf[c][k], k ? s[c][t] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+          for (int c = 0; c < CT; ++c) s[c][t] = mfma(f, qf[c][k], k ? s[c][t] : start_of<MODE>(slope[c], (float)(first + 16 * t + 4 * g - pos[c])));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -739,7 +763,7 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
       for (int i = 0; i < 16; ++i) v[c][i] = s[c][i / 4][i % 4];
       away[c] = (float)(first + 4 * g - pos[c]);
     }
-    score<MODE>(v, md, slope2, away, at);
+    score<MODE>(v, md, slope, away, at);
     uint4 pf[CT][2];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
@@ -862,7 +886,8 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a, int 
   __shared__ __attribute__((aligned(16))) uint4 lds[(2 * 4 * (HD / 32) + 2 * 2 * (HD / 16)) * 64];
   if (!made_for(a.plan, a.key)) return;
   const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
-  if (item < wide_items) many_columns<HD, MODE, TO>(a, item, kvh, lds);
+  if (item < wide_items && a.plan.w[kCols] == kQCols) many_columns<HD, MODE, TO, 3>(a, item, kvh, lds);
+  else if (item < wide_items) many_columns<HD, MODE, TO, 1>(a, item, kvh, lds);
   else few_columns<HD, MODE, TO>(a, item - wide_items, kvh, lds);
 }
 
@@ -879,7 +904,7 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a) {
     const int kvh = (int)(i % H_kv), at = (int)(i / H_kv), b = find_item(a.plan.split(), B, at), x = at - a.plan.split()[b];
     const int row0 = a.plan.row_start()[b], cols = a.plan.split()[b + 1] - a.plan.split()[b], halves = (a.plan.len()[b] + 63) / 64;
     const bool narrow = cols <= kNarrow;
-    const int shares = (halves - 1) / a.plan.w[narrow ? kNwChunk : kPfChunk] + 1, bc = narrow ? kNCols : kQCols;
+    const int shares = (halves - 1) / a.plan.w[narrow ? kNwChunk : kPfChunk] + 1, bc = narrow ? kNCols : a.plan.w[kCols];
     const int first = narrow ? a.plan.nws()[b] + x / bc * shares : a.plan.pf_of()[b] + ((cols - 1) / bc - x / bc) * shares;
     const int64_t part = ((int64_t)first * H_kv + kvh) * bc + x % bc, stride = (int64_t)H_kv * bc;
     const float* po = (narrow ? a.nw_o : a.part_o) + part * HD;

@@ -15,13 +15,13 @@ namespace page {
 constexpr int kTokens = 128;            // of a page
 constexpr int kMaxBatch = 4096;         // sequences: their prefix sums fit LDS
 constexpr int kMinExp = -100;           // least exponent of a scale: products of two of them and of a query stay normal numbers
-constexpr int kQCols = 384;             // (query, query head) columns of a prefill workgroup
-constexpr int kNarrow = 192;            // a sequence of up to so many columns goes to the kernel for few of them
-constexpr int kNCols = 32;              // columns of its workgroups
+// (query, query head) columns of a prefill workgroup: 384, or 128 where those of 384 would be fewer than kPfMany with less than kPfLong halves for each compute
+// unit; 32 of a sequence of up to kNarrow.  (A half of 64 tokens costs 384 columns 3 us and 128 1.6.)
+constexpr int kQCols = 384, kSCols = 128, kNCols = 32, kNarrow = 128, kPfMany = 320, kPfLong = 40;
 constexpr int kPfFill = 256;            // prefill workgroups that fill the chip, one to a compute unit: fewer are split over the keys
 
 // ---- plan: what grow leaves for the other kernels, int32 words.  Words 16 on: row_start, then the arrays below, each of batch + 1 words.
-enum { kStatus, kWideSeqs, kDecChunk, kDecItems, kPfChunk, kPfItems, kAppItems, kFree0, kBatch, kHq, kHkv, kMaxRows, kMagic, kNwChunk, kNwItems, kNwSlots, kHeadWords };
+enum { kStatus, kWideSeqs, kDecChunk, kDecItems, kPfChunk, kPfItems, kAppItems, kFree0, kBatch, kHq, kHkv, kMaxRows, kMagic, kNwChunk, kNwItems, kCols, kHeadWords };
 static_assert(kHeadWords == 16, "row_start's place is documented");
 constexpr int32_t kMagicWord = 0x45504732;
 struct Plan {
@@ -131,19 +131,38 @@ __device__ __forceinline__ void grow_row(const GrowArgs& a, int row, int b, int 
   if (a.pos) a.pos[row] = p;
 }
 
-// Sums over the block's threads, in every thread.
-template <int N, int NT> __device__ __forceinline__ void block_sums(int64_t (&v)[N], int64_t (*lds)[NT / 64]) {
+// Lane i gets the value of lane i - N of its row of 16, or with 0x142 / 0x143 rows 1 and 3 / 2 and 3 that of the last lane of row 0 and 2 / 1; else 0.
+template <int CTRL, int ROWS> __device__ __forceinline__ int32_t from_lower(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, CTRL < 0x140); }
+template <int CTRL, int ROWS> __device__ __forceinline__ double from_lower(double v) {
+  const int64_t b = __builtin_bit_cast(int64_t, v);
+  const uint32_t lo = from_lower<CTRL, ROWS>((int32_t)b), hi = from_lower<CTRL, ROWS>((int32_t)(b >> 32));
+  return __builtin_bit_cast(double, (int64_t)((uint64_t)hi << 32 | lo));
+}
+// Inclusive prefix sums over a wave; the last lane has the total.  (On the vector unit: through the LDS crossbar a step's scans took 4 us.)
+template <typename T> __device__ __forceinline__ T wave_prefix(T v) {
+  v += from_lower<0x111, 0xF>(v);
+  v += from_lower<0x112, 0xF>(v);
+  v += from_lower<0x114, 0xF>(v);
+  v += from_lower<0x118, 0xF>(v);
+  v += from_lower<0x142, 0xA>(v);
+  v += from_lower<0x143, 0xC>(v);
+  return v;
+}
+__device__ __forceinline__ double wave_total(double v) { return wave_prefix(v); }      // in lane 63
+
+// Sums over the block's threads, in every thread.  (In double: exact far beyond what is compared with them.)
+template <int N, int NT> __device__ __forceinline__ void block_sums(double (&v)[N], double (*lds)[NT / 64]) {
   constexpr int W = NT / 64;
   const int tid = threadIdx.x;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    for (int o = 32; o > 0; o >>= 1) v[i] += __shfl_xor(v[i], o, 64);
-    if ((tid & 63) == 0) lds[i][tid >> 6] = v[i];
+    v[i] = wave_total(v[i]);
+    if ((tid & 63) == 63) lds[i][tid >> 6] = v[i];
   }
   __syncthreads();
   static_assert(N * W <= NT && W <= 16, "a row of lanes per value");
   if (tid < N * W) {
-    int64_t x = lds[tid / W][tid % W];
+    double x = lds[tid / W][tid % W];
     for (int o = W / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, W);
     lds[tid / W][tid % W] = x;
   }
@@ -159,7 +178,7 @@ template <int N, int NT> __device__ __forceinline__ void block_scan(int32_t (&v)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(v[i], o, 64); if (lane >= o) v[i] += y; }
+    v[i] = wave_prefix(v[i]);
     if (lane == 63) lds[i][wave] = v[i];
   }
   __syncthreads();
@@ -177,12 +196,13 @@ template <int N, int NT> __device__ __forceinline__ void block_scan(int32_t (&v)
   __syncthreads();
 }
 
-// Columns of a sequence with n new rows, and the blocks that a prefill kernel cuts them into.
+// Columns of a sequence with n new rows, and the blocks of `many` columns, or of few, that prefill cuts them into.
 struct Cut { bool narrow; int blocks; };
-__device__ __forceinline__ Cut cut(int64_t n, int G) {
+__device__ __forceinline__ Cut cut(int64_t n, int G, int many) {
   const int64_t cols = n * G;
   const bool narrow = cols <= kNarrow;
-  return {narrow, (int)((cols + (narrow ? kNCols : kQCols) - 1) / (narrow ? kNCols : kQCols))};
+  const int c = narrow ? kNCols : many;
+  return {narrow, (int)((cols + c - 1) / c)};
 }
 
 // A length's place among 256, eight to a factor of two.
@@ -191,8 +211,8 @@ __device__ __forceinline__ int bucket(int t) { return (int)(__float_as_uint((flo
 // All or nothing: lengths, sums and chunk sizes by one workgroup, a thread per sequence.
 template <int NT>
 __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
-  constexpr int S = 8;
-  __shared__ int64_t red[S][NT / 64];
+  constexpr int S = 9;
+  __shared__ double red[S][NT / 64];
   __shared__ int32_t wsum[7][NT / 64], hist[256];
   __shared__ int32_t rows[NT + 1], lens[NT], fresh[NT];      // row_start, len, fresh, where the rows are looked at here
   const int tid = threadIdx.x, B = a.plan.n, G = a.H_q / a.H_kv;
@@ -202,62 +222,71 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
   if (tid < B) { first_l = a.len0[tid]; first_n = a.n_new[tid]; }
   const auto len_of = [&](int b) { return b == tid ? first_l : a.len0[b]; };
   const auto new_of = [&](int b) { return b == tid ? first_n : a.n_new[b]; };
-  // rows, new pages, 64-token halves of full pages; blocks of many columns and their halves, those of few; sequences of many; what is wrong
-  int64_t s[S] = {0, 0, 0, 0, 0, 0, 0, 0};
+  enum { Rows, Pages, FullHalves, Small, SmallHalves, Large, LargeHalves, Wide, NarrowHalves };      // blocks of 128 and 384 columns and what they see
+  double s[S] = {0, 0, 0, 0, 0, 0, 0, 0, 0};
+  int wrong = 0;
   for (int b = tid; b < B; b += NT) {
     const int64_t l = len_of(b), n = new_of(b);
-    if (l < 0 || l > cap || n < 0) { s[7] |= 1; continue; }
-    if (l + n > cap) { s[7] |= (int64_t)1 << 32; continue; }
-    const int64_t t = l + n;
-    const Cut c = cut(n, G);
-    s[0] += n; s[1] += t / kTokens - l / kTokens; s[2] += t / kTokens * 2;
-    if (c.narrow) s[5] += c.blocks * ((t + 63) / 64);
-    else { s[3] += c.blocks; s[4] += c.blocks * ((t + 63) / 64); s[6] += 1; }
+    if (l < 0 || l > cap || n < 0) { wrong |= 1; continue; }      // ECHOKV_PLAN_BAD_LENGTH
+    if (l + n > cap) { wrong |= 2; continue; }                    // ECHOKV_PLAN_TABLE_FULL
+    const int64_t t = l + n, seen = (t + 63) / 64;
+    const Cut c = cut(n, G, kSCols);
+    s[Rows] += n; s[Pages] += t / kTokens - l / kTokens; s[FullHalves] += t / kTokens * 2;
+    if (c.narrow) {
+      s[NarrowHalves] += (double)c.blocks * seen;
+    } else {
+      const int large = cut(n, G, kQCols).blocks;
+      s[Small] += c.blocks; s[SmallHalves] += (double)c.blocks * seen; s[Large] += large; s[LargeHalves] += (double)large * seen; s[Wide] += 1;
+    }
   }
   block_sums<S, NT>(s, red);
-  int status = 0;
-  if ((s[7] & 0xffffffff) || n_free0 < 0 || n_free0 > a.n_pages) status |= 1;      // ECHOKV_PLAN_BAD_LENGTH
-  if (s[7] >> 32) status |= 2;                                                     // ECHOKV_PLAN_TABLE_FULL
-  if (!status && s[1] > n_free0) status |= 4;                                      // ECHOKV_PLAN_NO_PAGES
-  if (!status && s[0] > a.max_rows) status |= 8;                                   // ECHOKV_PLAN_TOO_MANY_ROWS
+  int status = (__syncthreads_or(wrong & 1) ? 1 : 0) | (__syncthreads_or(wrong & 2) ? 2 : 0);
+  if (n_free0 < 0 || n_free0 > a.n_pages) status |= 1;
+  if (!status && s[Pages] > n_free0) status |= 4;      // ECHOKV_PLAN_NO_PAGES
+  if (!status && s[Rows] > a.max_rows) status |= 8;    // ECHOKV_PLAN_TOO_MANY_ROWS
   const bool ok = status == 0;
   if (!ok) {                                           // nobody grows: the halves of the lengths as they were
-    int64_t h[1] = {0};
+    double h[1] = {0};
     for (int b = tid; b < B; b += NT) { const int64_t l = len_of(b); if (l >= 0 && l <= cap) h[0] += l / kTokens * 2; }
     block_sums<1, NT>(h, red);
-    s[0] = s[1] = s[3] = s[4] = s[5] = s[6] = 0;
-    s[2] = h[0];
+    for (int i = 0; i < S; ++i) s[i] = 0;
+    s[FullHalves] = h[0];
   }
   // halves per item: as many for each of its waves (decode, few columns); of a share of the keys
-  const auto chunk = [](int64_t work, int items, int waves) { return (int)max((int64_t)waves, (work + (int64_t)items * waves - 1) / ((int64_t)items * waves) * waves); };
-  const int dec_chunk = chunk(s[2], a.dec_items, 4);
-  // Few columns: a block's last share is short, and one workgroup more than the chip holds at a time doubles the launch's time: of 1, 5/4, 6/4 and 7/4 times
-  // the even share, a wave each, the first that leaves no more items than that, else twice the even share.
-  int nw_chunk = chunk(s[5], a.nw_items, 8);
-  if (nw_chunk > 8) {
-    const int wave = tid >> 6, even = nw_chunk;
-    const auto candidate = [&](int k) { return (even * (4 + k) / 4 + 7) / 8 * 8; };
+  const auto chunk = [](double halves, int items, int waves) { const int64_t work = (int64_t)halves; return (int)max((int64_t)waves, (work + (int64_t)items * waves - 1) / ((int64_t)items * waves) * waves); };
+  const int dec_chunk = chunk(s[FullHalves], a.dec_items, 4);
+  const int wide = (int)s[Wide], total = (int)s[Rows];
+  const bool large = s[Large] * a.H_kv >= kPfMany || s[LargeHalves] * a.H_kv >= kPfFill * kPfLong;
+  const int many = large ? kQCols : kSCols;
+  const bool split = wide && (large ? s[Large] : s[Small]) * a.H_kv < kPfFill;
+  // A block's last share is short, and one workgroup more than the chip holds at a time doubles a launch's time: of 1, 5/4, 6/4 and 7/4 times the even share, a
+  // wave each, the first that leaves no more items than that, else twice the even share.
+  int nw_chunk = chunk(s[NarrowHalves], a.nw_items, 8), pf_chunk = 0x7fffffff;
+  for (int which = 0; which < 2; ++which) {
+    const bool narrow = which == 0;
+    const int unit = 8, slots = narrow ? a.nw_items : a.pf_items, even = narrow ? nw_chunk : chunk(large ? s[LargeHalves] : s[SmallHalves], a.pf_items, unit);
+    if (narrow ? even == unit : !split) continue;
+    const auto candidate = [&](int k) { return (even * (4 + k) / 4 + unit - 1) / unit * unit; };
+    const int wave = tid >> 6;
     if (wave < 4) {
       int64_t items = 0;
       for (int b = tid & 63; b < B; b += 64) {
         const int64_t n = a.n_new[b];
-        const Cut c = cut(n, G);
-        if (c.narrow && n) items += c.blocks * (((a.len0[b] + n + 63) / 64 - 1) / candidate(wave) + 1);
+        const Cut c = cut(n, G, many);
+        if (c.narrow == narrow && n) items += c.blocks * (((a.len0[b] + n + 63) / 64 - 1) / candidate(wave) + 1);
       }
       for (int o = 32; o > 0; o >>= 1) items += __shfl_xor(items, o, 64);
       if ((tid & 63) == 0) red[0][wave] = items;
     }
     __syncthreads();
     int k = 0;
-    while (k < 4 && red[0][k] > a.nw_items) ++k;
-    nw_chunk = candidate(k);
+    while (k < 4 && red[0][k] > slots) ++k;
+    (narrow ? nw_chunk : pf_chunk) = candidate(k);
     __syncthreads();
   }
-  const int pf_chunk = a.pf_items && s[3] * a.H_kv < kPfFill ? (int)max((int64_t)8, (s[4] + a.pf_items - 1) / a.pf_items) : 0x7fffffff;
-  const int wide = (int)s[6], total = (int)s[0];
   const auto wide_items = [&](int b) {                 // from the plan: the lengths may have been overwritten in place
     const int n = a.plan.row_start()[b + 1] - (b ? a.plan.row_start()[b] : 0), t = a.plan.len()[b];
-    const Cut c = cut(n, G);
+    const Cut c = cut(n, G, many);
     return c.narrow ? 0 : c.blocks * (((t + 63) / 64 - 1) / pf_chunk + 1);
   };
   int32_t carry[7] = {0, 0, 0, 0, 0, 0, 0};
@@ -271,7 +300,7 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
       a.len1[b] = ok ? l + n : (int)ll;
     }
     const int t = l + n, f0 = l / kTokens, f1 = t / kTokens, halves = f1 * 2, seen = (t + 63) / 64;
-    const Cut c = cut(n, G);
+    const Cut c = cut(n, G, many);
     const int shares = n > 0 ? (seen - 1) / (c.narrow ? nw_chunk : pf_chunk) + 1 : 0, few = c.narrow ? c.blocks * shares : 0;
     int32_t v[7];
     v[0] = n;
@@ -320,9 +349,9 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     int32_t* w = a.plan.w;
     for (int i : {0, 2, 3, 4, 5, 7, 8, 9}) a.plan.arr(i)[0] = 0;
     w[kStatus] = status; w[kWideSeqs] = wide; w[kDecChunk] = dec_chunk; w[kDecItems] = carry[2]; w[kPfChunk] = pf_chunk; w[kPfItems] = items[0];
-    w[kAppItems] = carry[1]; w[kFree0] = n_free0; w[kNwChunk] = nw_chunk; w[kNwItems] = carry[4]; w[kNwSlots] = carry[5];
+    w[kAppItems] = carry[1]; w[kFree0] = n_free0; w[kNwChunk] = nw_chunk; w[kNwItems] = carry[4]; w[kCols] = large ? kQCols : kSCols;
     w[kBatch] = B; w[kHq] = a.H_q; w[kHkv] = a.H_kv; w[kMaxRows] = a.max_rows; w[kMagic] = kMagicWord;
-    *a.n_free1 = n_free0 - (ok ? (int)s[1] : 0);
+    *a.n_free1 = n_free0 - (int)s[Pages];
     rows[0] = 0;
   }
   if (!a.rows_here) return;
@@ -333,12 +362,19 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
   }
 }
 
-__global__ __launch_bounds__(256) void grow_rows_kernel(GrowArgs a) {
-  const int row = blockIdx.x * 256 + threadIdx.x;
+constexpr int kRowsPerBlock = 256;
+__global__ __launch_bounds__(kRowsPerBlock) void grow_rows_kernel(GrowArgs a) {
+  __shared__ int32_t starts[kMaxBatch + 1];
   const int32_t* rs = a.plan.row_start();
-  if (row >= rs[a.plan.n]) return;
-  const int b = find_seq(rs, a.plan.n, row);
-  grow_row(a, row, b, rs[b], a.plan.len()[b], rs[b + 1] - rs[b], a.plan.fresh()[b], a.plan.w[kFree0]);
+  const int row0 = blockIdx.x * kRowsPerBlock, B = a.plan.n, total = rs[B];
+  if (row0 >= total) return;
+  for (int i = threadIdx.x; i <= B; i += kRowsPerBlock) starts[i] = rs[i];
+  __syncthreads();
+  const int n_free0 = a.plan.w[kFree0];
+  const int row = row0 + threadIdx.x;
+  if (row >= total) return;
+  const int b = find_seq(starts, B, row);
+  grow_row(a, row, b, starts[b], a.plan.len()[b], starts[b + 1] - starts[b], a.plan.fresh()[b], n_free0);
 }
 
 // ---- slots of any cached tokens
