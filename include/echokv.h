@@ -434,7 +434,11 @@ int echokv_prefill_attn_ex(const echokv_shape *shape, const echokv_layer_cache *
  *
  * One step of a batch:  echokv_pages_grow once, with the numbers of new tokens;
  * then per layer echokv_page_append and echokv_page_decode_attn or
- * echokv_page_prefill_attn, all with the plan that grow left. */
+ * echokv_page_prefill_attn, all with the plan that grow left.  Kernels and splits of
+ * the keys are chosen by the sizes of the whole step: the result of a sequence may
+ * differ in rounding with the other sequences of the batch.  A plan may be read by
+ * calls on several streams at once; each attention call in flight needs a workspace of
+ * its own, in which nothing has to start at zero. */
 #define ECHOKV_PAGE_TOKENS 128
 
 /* Block tables of a batch over a pool of pages, shared by the layers.  The caller
@@ -442,7 +446,7 @@ int echokv_prefill_attn_ex(const echokv_shape *shape, const echokv_layer_cache *
  * order and *n_free = n_pages; from then on grow and release keep them. */
 typedef struct {
   int32_t batch;      /* 1 .. 4096 */
-  int32_t max_pages;  /* full pages a sequence may hold, < 2^24; it may hold 127 tokens more */
+  int32_t max_pages;  /* full pages a sequence may hold, < 2^23; it may hold 127 tokens more */
   int32_t n_pages;    /* pages of the pool, < 2^24 */
   int32_t *table;     /* device [batch, max_pages] */
   int32_t *seq_len;   /* device [batch] */
@@ -522,7 +526,7 @@ int echokv_page_read(const echokv_shape *shape, const echokv_page_table *t,
 
 /* What may be done to the scores s_ij = scale * q_i . k_j (i, j positions) before the
  * softmax; NULL, or zeros and NULLs, for nothing:
- *   softcap    > 0: s <- softcap * tanh(s / softcap)
+ *   softcap    > 0 (1e-30 .. 1e37): s <- softcap * tanh(s / softcap)
  *   slopes     device [H_q] or NULL: then s <- s + slopes[h] * (j - i)
  *   prefix_len device [batch] or NULL (prefill): the tokens j < prefix_len[b] are seen
  *              by every query of the sequence, also by those in front of them; tokens

@@ -17,7 +17,7 @@ import numpy as np
 _LIB = None
 _call = None             # _hostcall.call or call_by_ctypes, and the addresses it is given, set by load()
 _APPEND = _WINDOW_APPEND = _DECODE = _DECODE_EX = 0
-_DTYPES = {}             # torch's dtypes by name
+_DTYPES = {}             # torch's dtypes by name, and the current GPU's number
 _PAGE = {}               # the paged cache's entry points: name -> address
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libechokv.so")
 
@@ -211,6 +211,7 @@ def load() -> C.CDLL:
     _APPEND, _WINDOW_APPEND = address(lib.echokv_cache_append), address(lib.echokv_window_append)
     _DECODE, _DECODE_EX = address(lib.echokv_decode_attn), address(lib.echokv_decode_attn_ex)
     _DTYPES.update((n, getattr(torch, n)) for n in ("uint8", "int32", "bfloat16", "float32"))
+    _DTYPES["device"] = torch._C._cuda_getDevice
     _PAGE.update((n, address(getattr(lib, "echokv_" + n))) for n in (
         "pages_grow", "pages_slots", "pages_release", "page_append", "page_read", "page_decode_attn", "page_prefill_attn"))
     _call = call
@@ -457,11 +458,11 @@ def augment_weights(shape: Shape, w_k, w_v, w_k_aug, w_v_aug, stream=None):
 
 # ---- paged 8-bit cache
 def _rows(t, dtype: str, least: int, what: str):
-    """Address of a tensor argument: contiguous, of the named torch dtype, at least so many elements.  An address passes as it is."""
+    """Address of a tensor argument: contiguous, on the current GPU, of the named torch dtype, at least so many elements.  An address passes as it is."""
     if t is None or type(t) is int:
         return t
     try:
-        if t.is_contiguous() and t.dtype is _DTYPES[dtype] and t.is_cuda and t.numel() >= least:
+        if t.is_contiguous() and t.dtype is _DTYPES[dtype] and t.numel() >= least and t.is_cuda and t.get_device() == _DTYPES["device"]():
             return t.data_ptr()
     except AttributeError:
         return _ptr(t)
@@ -471,7 +472,9 @@ def _rows(t, dtype: str, least: int, what: str):
         raise ValueError(f"{what}: not contiguous")
     if not t.is_cuda:
         raise ValueError(f"{what}: not on a GPU")
-    raise ValueError(f"{what}: {t.numel()} elements where {least} are needed")
+    if t.numel() < least:
+        raise ValueError(f"{what}: {t.numel()} elements where {least} are needed")
+    raise ValueError(f"{what}: on {t.device}, the current GPU is cuda:{_DTYPES['device']()}")
 
 
 class _Viewed:

@@ -35,7 +35,7 @@ int check_shape(const echokv_shape* s, Sizes* o) {
 int check_table(const echokv_page_table* t) {
   if (!t) return ECHOKV_ERR_NULL;
   if (t->batch <= 0 || t->max_pages <= 0 || t->n_pages <= 0) return ECHOKV_ERR_SHAPE;
-  if (t->batch > page::kMaxBatch || t->max_pages >= 1 << 24 || t->n_pages >= 1 << 24) return ECHOKV_ERR_UNSUPPORTED;
+  if (t->batch > page::kMaxBatch || t->max_pages >= 1 << 23 || t->n_pages >= 1 << 24) return ECHOKV_ERR_UNSUPPORTED;      // lengths below 2^30, slots below 2^31
   if (!t->table || !t->seq_len || !t->free_list || !t->n_free) return ECHOKV_ERR_NULL;
   return ECHOKV_OK;
 }
@@ -98,7 +98,7 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
               const echokv_score_extras* x, void* out, float* lse, const Schedule& s, page::AttnArgs* a) {
   if (!q || !out) return ECHOKV_ERR_NULL;
   if (!aligned16({q, out}) || ((uintptr_t)lse & 3)) return ECHOKV_ERR_SHAPE;
-  if (x && (!std::isfinite(x->softcap) || x->softcap < 0.f)) return ECHOKV_ERR_SHAPE;
+  if (x && (!std::isfinite(x->softcap) || x->softcap < 0.f || x->softcap > 1e37f || (x->softcap > 0.f && x->softcap < 1e-30f))) return ECHOKV_ERR_SHAPE;
   *a = page::AttnArgs{};
   a->k = (const uint8_t*)c->k; a->v = (const uint8_t*)c->v; a->ke = c->k_exp; a->ve = c->v_exp;
   a->kt = (const bf16_t*)c->k_tail; a->vt = (const bf16_t*)c->v_tail; a->q = (const bf16_t*)q;
@@ -228,6 +228,7 @@ int echokv_page_read(const echokv_shape* shape, const echokv_page_table* t, cons
   if (rc) return rc;
   if ((rc = check_table(t)) || (rc = check_cache(c))) return rc;
   if (n_rows < 0) return ECHOKV_ERR_SHAPE;
+  if (n_rows > 1 << 30) return ECHOKV_ERR_UNSUPPORTED;
   if (n_rows == 0) return ECHOKV_OK;
   if (!row_slot || !k_out || !v_out) return ECHOKV_ERR_NULL;
   if (!aligned16({k_out, v_out})) return ECHOKV_ERR_SHAPE;

@@ -131,9 +131,9 @@ template <typename TO> __device__ __forceinline__ void put4(TO* p, float4 v) {
 // Four dims of a finished row, and with the first four its log-sum-exp; a row that sees nothing: zeros and -inf.
 template <int HD, typename TO>
 __device__ __forceinline__ void finish(const AttnArgs& a, int64_t row, int d4, float4 acc, float M, float sum) {
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   put4(reinterpret_cast<TO*>(a.out) + row * HD + d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-  if (a.lse && d4 == 0) a.lse[row] = sum > 0.f ? (M + __log2f(sum)) * kLn2 : -INFINITY;
+  if (a.lse && d4 == 0) a.lse[row] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * kLn2;
 }
 
 // Four dims of column c from the four waves' softmaxes of their own.
@@ -660,11 +660,11 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
     const int x = w0 + off, qi = x / G;
     const int64_t row = (int64_t)(row0 + qi) * H_q + kvh * G + (x - qi * G);
     if (shares == 1) {
-      const float inv = sum > 0.f ? 1.f / sum : 0.f;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
       for (int u = 0; u < U; ++u)
         put4(reinterpret_cast<TO*>(a.out) + row * HD + 16 * u + 4 * g, make_float4(o[c][u][0] * inv, o[c][u][1] * inv, o[c][u][2] * inv, o[c][u][3] * inv));
-      if (a.lse && g == 0) a.lse[row] = sum > 0.f ? (m[c] + __log2f(sum)) * kLn2 : -INFINITY;
+      if (a.lse && g == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m[c] + __log2f(sum)) * kLn2;
     } else {
       const int64_t part = ((int64_t)item * a.key.H_kv + kvh) * QC + (x - x0);
 #pragma unroll

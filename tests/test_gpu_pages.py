@@ -273,6 +273,83 @@ def test_caps_far_below_and_above_the_scores(cap):
         b.check(out[i:i + 1], lse[i:i + 1], q[i:i + 1], i, [n - 1], P_PAIR, cap if cap < 10 else 0.0)       # 1e6: (s / cap)^2 / 3 is nothing
 
 
+@pytest.mark.parametrize("cap", [60.0, 12.0, 3.0])
+def test_prefill_and_decode_with_scores_below_a_third_of_the_cap_three_quarters_and_beyond(cap):
+    """One form of the cap for each; largest score of a wave's 64 x 48 about 16."""
+    b = Batch(GQA, 2).grow([700, 130])
+    q = b.random(830, b.hq, b.d, scale=3.0)
+    out, lse = b.prefill(q, softcap=cap)
+    at = 0
+    for i, n in enumerate((700, 130)):
+        b.check(out[at:at + n], lse[at:at + n], q[at:at + n], i, list(range(n)), P_ONE, cap)
+        at += n
+    out, lse = b.decode(q[:2], softcap=cap)
+    for i, n in enumerate((700, 130)):
+        b.check(out[i:i + 1], lse[i:i + 1], q[i:i + 1], i, [n - 1], P_PAIR, cap)
+
+
+def test_long_chunks_and_many_blocks():
+    """Blocks of 384 columns, whole and with keys split, beside a sequence of few columns: some rows of each."""
+    for layer, ctx, new, n_pages in (((16, 8, 64), (0, 100, 0), (6200, 3, 77), 60), ((8, 1, 64), (0, 41000, 500), (0, 260, 20), 400)):
+        b = Batch(layer, 3, max_pages=330, n_pages=n_pages)
+        if any(ctx):
+            b.grow(ctx)
+        b.grow(new)
+        q = b.random(sum(new), b.hq, b.d)
+        out, lse = b.prefill(q)
+        at = 0
+        for i, (c, n) in enumerate(zip(ctx, new)):
+            for r in sorted({0, 1, n // 3, n // 2, n - 130, n - 1}):
+                if 0 <= r < n:
+                    b.check(out[at + r:at + r + 1], lse[at + r:at + r + 1], q[at + r:at + r + 1], i, [c + r], P_ONE)
+            at += n
+
+
+def test_a_query_of_nan_stays_alone():
+    b = Batch(GQA, 1).grow([500])
+    q = b.random(500, b.hq, b.d)
+    clean, clean_lse = b.prefill(q)
+    q[77, 3] = float("nan")
+    out, lse = b.prefill(q)
+    assert torch.isnan(out[77, 3]).all() and torch.isnan(lse[77, 3])
+    out[77, 3], lse[77, 3] = clean[77, 3], clean_lse[77, 3]
+    assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+
+
+def test_a_plan_of_another_step_does_nothing():
+    """Shapes of other head counts, another max_rows, a buffer that no step has written."""
+    b = Batch(GQA, 2).grow([300, 40])
+    q = b.random(340, b.hq, b.d).to(DEV)
+    k = torch.ones(340, 256, dtype=torch.bfloat16, device=DEV)
+    before = b.cache.k_tail.clone()
+    wide = ek.make_shape(16, 2, 128, 0, "bf16")
+    other = ek.PagePlan(b.plan.buf, 2, 339)
+    blank = ek.PagePlan(torch.zeros_like(b.plan.buf), 2, 340)
+    for shape, plan in ((wide, b.plan), (b.shape, other), (b.shape, blank)):
+        out = torch.full((340, shape.n_q_heads, 128), 3.0, dtype=torch.bfloat16, device=DEV)
+        ws = torch.empty(ek.page_workspace_bytes(shape, 2, plan.max_rows), dtype=torch.uint8, device=DEV)
+        qq = q.repeat_interleave(shape.n_q_heads // 8, 1)
+        ek.page_decode_attn(shape, b.table, b.cache, plan, qq, out, None, ws)
+        ek.page_prefill_attn(shape, b.table, b.cache, plan, qq, out, None, ws)
+        ek.page_append(shape, b.table, b.cache, plan, k, k)
+        assert (out == 3.0).all() and torch.equal(torch.nan_to_num(b.cache.k_tail.float()), torch.nan_to_num(before.float()))
+
+
+def test_two_calls_at_once_share_a_plan():
+    b = Batch(GQA, 3).grow([3000, 700, 129])
+    q = [b.random(3, b.hq, b.d).to(DEV) for _ in range(2)]
+    want = [b.decode(x) for x in q]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs, ws = [b.out(3) for _ in range(2)], [b.workspace() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            ek.page_decode_attn(b.shape, b.table, b.cache, b.plan, q[i], *outs[i], ws[i], stream=st)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(outs[i][0].cpu(), want[i][0]) and torch.equal(outs[i][1].cpu(), want[i][1])
+
+
 PREFILL = {"one": ([0], [1]), "short": ([0, 5], [17, 3]), "page": ([0, 128, 100], [128, 128, 28]), "odd": ([0, 200, 0, 131], [301, 77, 0, 1]),
            "behind": ([2500, 10, 0], [3, 40, 129]), "blocks": ([0, 70], [900, 390])}
 

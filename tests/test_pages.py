@@ -101,7 +101,7 @@ def test_shapes(shape, want):
 
 @pytest.mark.parametrize("change,want", [
     (dict(batch=0), ek.ERR_SHAPE), (dict(max_pages=0), ek.ERR_SHAPE), (dict(n_pages=-1), ek.ERR_SHAPE), (dict(batch=4097), ek.ERR_UNSUPPORTED),
-    (dict(n_pages=1 << 24), ek.ERR_UNSUPPORTED), (dict(max_pages=1 << 24), ek.ERR_UNSUPPORTED), (dict(table=None), ek.ERR_NULL),
+    (dict(n_pages=1 << 24), ek.ERR_UNSUPPORTED), (dict(max_pages=1 << 23), ek.ERR_UNSUPPORTED), (dict(table=None), ek.ERR_NULL),
     (dict(seq_len=None), ek.ERR_NULL), (dict(free_list=None), ek.ERR_NULL), (dict(n_free=None), ek.ERR_NULL)])
 def test_tables(change, want):
     every = SHAPED + ("slots", "release")
@@ -129,7 +129,7 @@ def test_rows_queries_outputs_and_workspaces():
     assert codes(("append",) + ATTN, ptr=FAKE + 2) == {n: ek.ERR_SHAPE for n in ("append",) + ATTN}
     assert codes(("read",) + ATTN, out=None) == {n: ek.ERR_NULL for n in ("read",) + ATTN}
     assert codes(("read",) + ATTN, out=FAKE + 2) == {n: ek.ERR_SHAPE for n in ("read",) + ATTN}
-    for cap in (-1.0, float("inf"), float("nan")):
+    for cap in (-1.0, float("inf"), float("nan"), 1e-31, 2e37):
         assert codes(ATTN, softcap=cap) == {n: ek.ERR_SHAPE for n in ATTN}
     assert codes(ATTN) == {n: ek.ERR_WORKSPACE for n in ATTN}
     need = ek.page_workspace_bytes(SHAPE, 2, 10)
@@ -149,6 +149,22 @@ def test_the_binding_checks_tensors():
         ek.pages_release(Table(), t.long())
     with pytest.raises(ValueError, match="not contiguous"):
         ek.pages_release(Table(), t.T[1:])
+
+
+def test_views_follow_their_tensors():
+    class T:                                                 # a tensor's address and shape
+        def __init__(self, p, *shape): self.p, self.shape = p, shape
+        def data_ptr(self): return self.p
+    t = ek.PageTable(T(FAKE, 3, 7), T(FAKE + 64, 3), T(FAKE + 128, 9), T(FAKE + 192, 1))
+    c = t.as_c()
+    assert (c.batch, c.max_pages, c.n_pages, c.table, c.n_free) == (3, 7, 9, FAKE, FAKE + 192) and t.as_c() is c
+    t.seq_len.p = FAKE + 256                                 # other storage behind the same tensor
+    assert t.as_c() is not c and t.as_c().seq_len == FAKE + 256
+    t.free_list = T(FAKE + 320, 11)
+    assert t.as_c().n_pages == t.n_pages == 11 and t.as_c().free_list == FAKE + 320
+    cache = ek.PageCache(*(T(FAKE + 64 * i, 9) for i in range(6)))
+    a = cache.as_c(SHAPE, t)
+    assert cache.as_c(SHAPE, t) is a and cache.as_c(ek.make_shape(8, 4, 128, 0, "bf16"), t) is not a
 
 
 def test_reference_rounding_and_scales():
