@@ -405,6 +405,9 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(AttnArgs a) {
   join<HD, TO>(a, a.part_o + first * HD, a.part_ml + first * 2, n, H_q, row);
 }
 
+// Shares of `chunk` halves that the first `tokens` of a sequence fill.
+__device__ __forceinline__ int parts_of(int tokens, int chunk) { return ((tokens + 63) / 64 - 1) / chunk + 1; }
+
 // ---- prefill: the queries of the new tokens.  A workgroup of eight waves takes 384 columns (query, query head of the KV head) of one sequence,
 // 48 to a wave, and walks the 64-token halves of the keys they see: codes to registers, widened to bf16 on their way into LDS
 // (once for all eight waves), operands back in the order of the lanes.  Two buffers, one barrier per half.  Where few blocks of queries face
@@ -449,7 +452,7 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
   const int H_q = a.key.H_q, G = a.G;
   const int rank = find_item(a.plan.pf(), a.plan.w[kWideSeqs], item), item0 = a.plan.pf()[rank], b = __builtin_amdgcn_readfirstlane(a.plan.order()[rank]);
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
-  const int chunk = a.plan.w[kPfChunk], shares = ((len + 63) / 64 - 1) / chunk + 1;
+  const int chunk = a.plan.w[kPfChunk], shares = parts_of(len, chunk);
   const int cols = n * G;                   // (below 2^31: the host sees to it)
   const int blocks = (cols - 1) / QC + 1, j = item - item0, share = j % shares;
   const int x0 = (blocks - 1 - j / shares) * QC;    // the longest ones first
@@ -457,8 +460,9 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
   const int full_halves = len / kTokens * 2, tail_rows = len % kTokens;
   // what the block and the wave see: keys up to their last column's own, or the prefix
   const int xl = min(x0, cols - QC) + QC - 1;
-  const int seen = max(len0 + xl / G + 1, prefix);
-  const int h0 = share * min(chunk, 0x3fffffff), h1 = min((seen + 63) / 64, shares > 1 ? h0 + chunk : 0x7fffffff);
+  const int seen = max(len0 + xl / G + 1, prefix), parts = parts_of(seen, chunk);
+  if (share >= parts) return;
+  const int h0 = share * min(chunk, 0x3fffffff), h1 = min((seen + 63) / 64, parts > 1 ? h0 + chunk : 0x7fffffff);
   const int w0 = min(x0 + wave * (16 * CT), cols);      // (cols: none of the wave's columns exists)
   const bool active = w0 < cols;
   const int wave_first = len0 + min(w0, cols - 1) / G;         // position of the wave's first column
@@ -659,7 +663,7 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
     if (off >= cols - w0) continue;
     const int x = w0 + off, qi = x / G;
     const int64_t row = (int64_t)(row0 + qi) * H_q + kvh * G + (x - qi * G);
-    if (shares == 1) {
+    if (parts == 1) {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -686,12 +690,13 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
   if (item >= a.plan.w[kNwItems]) return;
   const int H_q = a.key.H_q, G = a.G, b = find_item(a.plan.nw(), a.key.batch, item), j = item - a.plan.nw()[b];
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
-  const int chunk = a.plan.w[kNwChunk], halves = (len + 63) / 64, shares = (halves - 1) / chunk + 1, share = j % shares;
+  const int chunk = a.plan.w[kNwChunk], shares = parts_of(len, chunk), share = j % shares;
   const int cols = n * G, x0 = j / shares * kNCols, nc = min(kNCols, cols - x0);
   const int prefix = a.prefix ? min(max(a.prefix[b], 0), len) : 0;
   const int full_halves = len / kTokens * 2, tail_rows = len % kTokens;
   const int block_first = len0 + x0 / G, seen = max(len0 + (x0 + nc - 1) / G + 1, prefix);
-  const int begin = share * chunk, end = min(begin + chunk, (seen + 63) / 64);
+  const int begin = share * chunk, end = min(begin + chunk, (seen + 63) / 64), parts = parts_of(seen, chunk);
+  if (share >= parts) return;
 
   uint4 qf[CT][KS];
   int pos[CT];
@@ -842,7 +847,7 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
   }
   for (; hf < end; hf += kPfWaves) half(hf, 0, false, std::false_type{});
 
-  const int slot = shares > 1 ? a.plan.nws()[b] + j : 0;
+  const int slot = parts > 1 ? a.plan.nws()[b] + j : 0;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     const float sum1 = rows_sum(l[c]);
@@ -868,7 +873,7 @@ __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh
       const int k = x / (HD / 4), d4 = x % (HD / 4) * 4;
       float M, sum;
       const float4 acc = join_waves<HD>(jn.so, jn.sm, jn.sl, k, d4, M, sum);
-      if (shares == 1) {
+      if (parts == 1) {
         const int col = x0 + 16 * c + k, qi = col / G;
         const int64_t row = (int64_t)(row0 + qi) * H_q + kvh * G + (col - qi * G);
         finish<HD, TO>(a, row, d4, acc, M, sum);
@@ -902,27 +907,31 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a) {
   const bool whole = units <= kMergeBlocks;
   for (int64_t i = whole ? blockIdx.x : blockIdx.x * 4 + wave; i < units; i += whole ? gridDim.x : gridDim.x * 4) {
     const int kvh = (int)(i % H_kv), at = (int)(i / H_kv), b = find_item(a.plan.split(), B, at), x = at - a.plan.split()[b];
-    const int row0 = a.plan.row_start()[b], cols = a.plan.split()[b + 1] - a.plan.split()[b], halves = (a.plan.len()[b] + 63) / 64;
+    const int row0 = a.plan.row_start()[b], cols = a.plan.split()[b + 1] - a.plan.split()[b], len = a.plan.len()[b];
     const bool narrow = cols <= kNarrow;
-    const int shares = (halves - 1) / a.plan.w[narrow ? kNwChunk : kPfChunk] + 1, bc = narrow ? kNCols : a.plan.w[kCols];
+    const int chunk = a.plan.w[narrow ? kNwChunk : kPfChunk], shares = parts_of(len, chunk), bc = narrow ? kNCols : a.plan.w[kCols];
+    // what the column's block sees, hence its parts: a block of one is finished already
+    const int last = min(x / bc * bc, cols - bc) + bc - 1, seen = max(len - cols / a.G + last / a.G + 1, a.prefix ? min(a.prefix[b], len) : 0);
+    const int parts = parts_of(seen, chunk);
+    if (parts == 1) continue;
     const int first = narrow ? a.plan.nws()[b] + x / bc * shares : a.plan.pf_of()[b] + ((cols - 1) / bc - x / bc) * shares;
     const int64_t part = ((int64_t)first * H_kv + kvh) * bc + x % bc, stride = (int64_t)H_kv * bc;
     const float* po = (narrow ? a.nw_o : a.part_o) + part * HD;
     const float* pml = (narrow ? a.nw_ml : a.part_ml) + part * 2;
     const int64_t row = (int64_t)(row0 + x / a.G) * a.key.H_q + kvh * a.G + x % a.G;
     if (whole) {
-      join<HD, TO>(a, po, pml, shares, stride, row);
+      join<HD, TO>(a, po, pml, parts, stride, row);
       __syncthreads();
       continue;
     }
     const int d4 = lane % L * 4, gr = lane / L;
     float M = kNoScore;
-    for (int k = lane; k < shares; k += 64) M = fmaxf(M, pml[k * stride * 2]);
+    for (int k = lane; k < parts; k += 64) M = fmaxf(M, pml[k * stride * 2]);
     M = wave_max64(M);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
 #pragma unroll 4
-    for (int k = gr; k < shares; k += GR) {
+    for (int k = gr; k < parts; k += GR) {
       const float2 ml = *reinterpret_cast<const float2*>(pml + k * stride * 2);
       const float4 y = *reinterpret_cast<const float4*>(po + k * stride * HD + d4);
       const float f = __builtin_amdgcn_exp2f(ml.x - M);

@@ -222,7 +222,7 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
   if (tid < B) { first_l = a.len0[tid]; first_n = a.n_new[tid]; }
   const auto len_of = [&](int b) { return b == tid ? first_l : a.len0[b]; };
   const auto new_of = [&](int b) { return b == tid ? first_n : a.n_new[b]; };
-  enum { Rows, Pages, FullHalves, Small, SmallHalves, Large, LargeHalves, Wide, NarrowHalves };      // blocks of 128 and 384 columns and what they see
+  enum { Rows, Pages, FullHalves, Small, SmallHalves, Large, LargeHalves, Wide, NarrowHalves };      // blocks of 128 and 384 columns, what they see at most
   double s[S] = {0, 0, 0, 0, 0, 0, 0, 0, 0};
   int wrong = 0;
   for (int b = tid; b < B; b += NT) {
