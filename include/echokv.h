@@ -426,7 +426,8 @@ int echokv_prefill_attn_ex(const echokv_shape *shape, const echokv_layer_cache *
  * were given: keys of a model with rotary embedding come in rotated.
  *
  * bf16 rows and queries (shape->dtype), head_dim 64 or 128, flags == 0, otherwise
- * ECHOKV_ERR_UNSUPPORTED; n_retained is not used.  Pointers to rows, pages, tails,
+ * ECHOKV_ERR_UNSUPPORTED; n_retained is not used, a softmax_scale that is given
+ * lies in 1e-10 .. 1e10 (ECHOKV_ERR_SHAPE).  Pointers to rows, pages, tails,
  * queries, outputs, plans and workspaces are 16-byte aligned (ECHOKV_ERR_SHAPE, for
  * the last two ECHOKV_ERR_WORKSPACE).  Everything that depends on lengths is read
  * on the device: all calls can be captured in a graph, and a replayed step follows
@@ -438,7 +439,8 @@ int echokv_prefill_attn_ex(const echokv_shape *shape, const echokv_layer_cache *
  * the keys are chosen by the sizes of the whole step: the result of a sequence may
  * differ in rounding with the other sequences of the batch.  A plan may be read by
  * calls on several streams at once; each attention call in flight needs a workspace of
- * its own, in which nothing has to start at zero. */
+ * its own, in which nothing has to start at zero; outputs and workspaces overlap
+ * nothing else. */
 #define ECHOKV_PAGE_TOKENS 128
 
 /* Block tables of a batch over a pool of pages, shared by the layers.  The caller
@@ -526,7 +528,7 @@ int echokv_page_read(const echokv_shape *shape, const echokv_page_table *t,
 
 /* What may be done to the scores s_ij = scale * q_i . k_j (i, j positions) before the
  * softmax; NULL, or zeros and NULLs, for nothing:
- *   softcap    > 0 (1e-30 .. 1e37): s <- softcap * tanh(s / softcap)
+ *   softcap    > 0 (1e-20 .. 1e20): s <- softcap * tanh(s / softcap)
  *   slopes     device [H_q] or NULL: then s <- s + slopes[h] * (j - i)
  *   prefix_len device [batch] or NULL (prefill): the tokens j < prefix_len[b] are seen
  *              by every query of the sequence, also by those in front of them; tokens

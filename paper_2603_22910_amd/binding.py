@@ -457,12 +457,21 @@ def augment_weights(shape: Shape, w_k, w_v, w_k_aug, w_v_aug, stream=None):
 
 
 # ---- paged 8-bit cache
-def _rows(t, dtype: str, least: int, what: str):
-    """Address of a tensor argument: contiguous, on the current GPU, of the named torch dtype, at least so many elements.  An address passes as it is."""
+def _gpu() -> int:
+    """The current GPU's number; without any one that no tensor has."""
+    try:
+        return _DTYPES["device"]()
+    except (KeyError, RuntimeError):
+        return -2
+
+
+def _rows(t, dtype: str, least: int, what: str, on: Optional[int] = None):
+    """Address of a tensor argument: contiguous, on the current GPU (on, where that is known), of the named torch dtype, at least so many elements.  An
+    address passes as it is."""
     if t is None or type(t) is int:
         return t
     try:
-        if t.is_contiguous() and t.dtype is _DTYPES[dtype] and t.numel() >= least and t.is_cuda and t.get_device() == _DTYPES["device"]():
+        if t.is_contiguous() and t.dtype is _DTYPES[dtype] and t.numel() >= least and t.get_device() == (_gpu() if on is None else on):
             return t.data_ptr()
     except AttributeError:
         return _ptr(t)
@@ -474,13 +483,27 @@ def _rows(t, dtype: str, least: int, what: str):
         raise ValueError(f"{what}: not on a GPU")
     if t.numel() < least:
         raise ValueError(f"{what}: {t.numel()} elements where {least} are needed")
-    raise ValueError(f"{what}: on {t.device}, the current GPU is cuda:{_DTYPES['device']()}")
+    raise ValueError(f"{what}: on {t.device}, the current GPU is cuda:{_gpu()}")
+
+
+def _space(t, on: int):
+    """Address and bytes of a workspace."""
+    if t is None:
+        return None, 0
+    try:
+        if t.get_device() != on:
+            raise ValueError(f"workspace: on {t.device}, the current GPU is cuda:{on}")
+        if not t.is_contiguous():
+            raise ValueError("workspace: not contiguous")
+    except AttributeError:                 # something else with an address and a size
+        pass
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 class _Viewed:
-    """Tensors with a C view of them that is made once: a decode loop needs it in every call of every layer.  It is made again when an
-    attribute is set or a tensor's address has changed (its storage can be replaced)."""
-    _view = _at = None
+    """Tensors with a C view of them that is made once: a decode loop needs it in every call of every layer.  It is made again, with its checks, when an
+    attribute is set, a tensor's address has changed (its storage can be replaced) or another GPU is the current one."""
+    _view = _at = _on = None
 
     def __setattr__(self, name, value):
         self.__dict__[name] = value
@@ -488,9 +511,10 @@ class _Viewed:
 
     def _viewed(self, at, make):
         d = self.__dict__
-        if d["_view"] is None or at != self._at:
+        on = _gpu()
+        if d["_view"] is None or at != self._at or on != self._on:
             view = make()
-            d["_at"], d["_view"] = at, view
+            d["_at"], d["_on"], d["_view"] = at, on, view
         return d["_view"]
 
 
@@ -595,33 +619,37 @@ def pages_grow(shape: Shape, table: PageTable, n_new, plan: PagePlan, seq_len_ou
                stream=None):
     """seq_len_out, n_free_out: the table's own arrays unless given."""
     load()
+    on = _gpu()
     b = table.batch
-    _check(_call(_PAGE["pages_grow"], _shape(shape), table.as_c(), _rows(n_new, "int32", b, "n_new"),
-                 _rows(table.seq_len if seq_len_out is None else seq_len_out, "int32", b, "seq_len_out"),
-                 _rows(table.n_free if n_free_out is None else n_free_out, "int32", 1, "n_free_out"),
-                 _rows(row_slot, "int32", plan.max_rows, "row_slot"), _rows(row_pos, "int32", plan.max_rows, "row_pos"), plan.as_c(),
+    _check(_call(_PAGE["pages_grow"], _shape(shape), table.as_c(), _rows(n_new, "int32", b, "n_new", on),
+                 _rows(table.seq_len if seq_len_out is None else seq_len_out, "int32", b, "seq_len_out", on),
+                 _rows(table.n_free if n_free_out is None else n_free_out, "int32", 1, "n_free_out", on),
+                 _rows(row_slot, "int32", plan.max_rows, "row_slot", on), _rows(row_pos, "int32", plan.max_rows, "row_pos", on), plan.as_c(),
                  _stream(stream)), "echokv_pages_grow")
 
 
 def pages_slots(table: PageTable, row_start, first_pos, row_slot, n_rows: Optional[int] = None, stream=None):
     load()
+    on = _gpu()
     n = int(row_slot.shape[0] if n_rows is None else n_rows)
-    _check(_call(_PAGE["pages_slots"], table.as_c(), _rows(row_start, "int32", table.batch + 1, "row_start"),
-                 _rows(first_pos, "int32", table.batch, "first_pos"), n, _rows(row_slot, "int32", n, "row_slot"), _stream(stream)),
+    _check(_call(_PAGE["pages_slots"], table.as_c(), _rows(row_start, "int32", table.batch + 1, "row_start", on),
+                 _rows(first_pos, "int32", table.batch, "first_pos", on), n, _rows(row_slot, "int32", n, "row_slot", on), _stream(stream)),
            "echokv_pages_slots")
 
 
 def pages_release(table: PageTable, which, stream=None):
     load()
-    _check(_call(_PAGE["pages_release"], table.as_c(), _rows(which, "int32", table.batch, "which"), _stream(stream)), "echokv_pages_release")
+    on = _gpu()
+    _check(_call(_PAGE["pages_release"], table.as_c(), _rows(which, "int32", table.batch, "which", on), _stream(stream)), "echokv_pages_release")
 
 
 def page_append(shape: Shape, table: PageTable, cache: PageCache, plan: PagePlan, k_new, v_new, stream=None):
     """k_new, v_new: bf16 [max_rows, n_kv_heads * d]; those behind the step's rows are not read."""
     load()
+    on = _gpu()
     least = plan.max_rows * shape.n_kv_heads * shape.head_dim
-    _check(_call(_PAGE["page_append"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(), _rows(k_new, "bfloat16", least, "k_new"),
-                 _rows(v_new, "bfloat16", least, "v_new"), _stream(stream)), "echokv_page_append")
+    _check(_call(_PAGE["page_append"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(), _rows(k_new, "bfloat16", least, "k_new", on),
+                 _rows(v_new, "bfloat16", least, "v_new", on), _stream(stream)), "echokv_page_append")
 
 
 _OUT = {BF16: "bfloat16", F32: "float32"}
@@ -629,39 +657,42 @@ _OUT = {BF16: "bfloat16", F32: "float32"}
 
 def page_read(shape: Shape, table: PageTable, cache: PageCache, row_slot, k_out, v_out, n_rows: Optional[int] = None, stream=None):
     load()
+    on = _gpu()
     n = int(row_slot.shape[0] if n_rows is None else n_rows)
     least, dtype = n * shape.n_kv_heads * shape.head_dim, _OUT.get(shape.out_dtype, "float32")
-    _check(_call(_PAGE["page_read"], _shape(shape), table.as_c(), cache.as_c(shape, table), _rows(row_slot, "int32", n, "row_slot"), n,
-                 _rows(k_out, dtype, least, "k_out"), _rows(v_out, dtype, least, "v_out"), _stream(stream)), "echokv_page_read")
+    _check(_call(_PAGE["page_read"], _shape(shape), table.as_c(), cache.as_c(shape, table), _rows(row_slot, "int32", n, "row_slot", on), n,
+                 _rows(k_out, dtype, least, "k_out", on), _rows(v_out, dtype, least, "v_out", on), _stream(stream)), "echokv_page_read")
 
 
-def _score_extras(shape: Shape, table: PageTable, softcap, slopes, prefix_len) -> Optional[ScoreExtras]:
+def _score_extras(shape: Shape, table: PageTable, softcap, slopes, prefix_len, on) -> Optional[ScoreExtras]:
     if not softcap and slopes is None and prefix_len is None:
         return None
-    return ScoreExtras(float(softcap), _rows(slopes, "float32", shape.n_q_heads, "slopes"), _rows(prefix_len, "int32", table.batch, "prefix_len"))
+    return ScoreExtras(float(softcap), _rows(slopes, "float32", shape.n_q_heads, "slopes", on), _rows(prefix_len, "int32", table.batch, "prefix_len", on))
 
 
 def page_decode_attn(shape: Shape, table: PageTable, cache: PageCache, plan: PagePlan, q, out, lse_out, workspace, softcap: float = 0.0,
                      slopes=None, stream=None):
     """slopes: float32 [n_q_heads] on the GPU."""
     load()
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    on = _gpu()
+    space, nbytes = _space(workspace, on)
     rows = table.batch * shape.n_q_heads
     _check(_call(_PAGE["page_decode_attn"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(),
-                 _rows(q, "bfloat16", rows * shape.head_dim, "q"), _score_extras(shape, table, softcap, slopes, None),
-                 _rows(out, _OUT.get(shape.out_dtype, "float32"), rows * shape.head_dim, "out"), _rows(lse_out, "float32", rows, "lse_out"),
-                 _ptr(workspace), nbytes, _stream(stream)), "echokv_page_decode_attn")
+                 _rows(q, "bfloat16", rows * shape.head_dim, "q", on), _score_extras(shape, table, softcap, slopes, None, on),
+                 _rows(out, _OUT.get(shape.out_dtype, "float32"), rows * shape.head_dim, "out", on), _rows(lse_out, "float32", rows, "lse_out", on),
+                 space, nbytes, _stream(stream)), "echokv_page_decode_attn")
 
 
 def page_prefill_attn(shape: Shape, table: PageTable, cache: PageCache, plan: PagePlan, q, out, lse_out, workspace, softcap: float = 0.0,
                       slopes=None, prefix_len=None, stream=None):
     """q, out: [max_rows, n_q_heads, d], lse_out [max_rows, n_q_heads]; slopes: float32 [n_q_heads], prefix_len: int32 [batch], both on the GPU."""
     load()
+    on = _gpu()
     rows = plan.max_rows * shape.n_q_heads
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_call(_PAGE["page_prefill_attn"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(), _rows(q, "bfloat16", rows * shape.head_dim, "q"),
-                 _score_extras(shape, table, softcap, slopes, prefix_len), _rows(out, _OUT.get(shape.out_dtype, "float32"), rows * shape.head_dim, "out"),
-                 _rows(lse_out, "float32", rows, "lse_out"), _ptr(workspace), nbytes, _stream(stream)), "echokv_page_prefill_attn")
+    space, nbytes = _space(workspace, on)
+    _check(_call(_PAGE["page_prefill_attn"], _shape(shape), table.as_c(), cache.as_c(shape, table), plan.as_c(), _rows(q, "bfloat16", rows * shape.head_dim, "q", on),
+                 _score_extras(shape, table, softcap, slopes, prefix_len, on), _rows(out, _OUT.get(shape.out_dtype, "float32"), rows * shape.head_dim, "out", on),
+                 _rows(lse_out, "float32", rows, "lse_out", on), space, nbytes, _stream(stream)), "echokv_page_prefill_attn")
 
 
 def profile_stream_read(buf, repeats: int = 5) -> float:

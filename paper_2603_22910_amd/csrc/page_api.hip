@@ -29,7 +29,8 @@ int check_shape(const echokv_shape* s, Sizes* o) {
   if (s->dtype != ECHOKV_BF16 || s->flags) return ECHOKV_ERR_UNSUPPORTED;
   *o = {s->n_q_heads, s->n_kv_heads, s->n_q_heads / s->n_kv_heads, s->head_dim, s->n_kv_heads * s->head_dim, s->out_dtype == ECHOKV_BF16,
         s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / std::sqrt((float)s->head_dim)};
-  return ECHOKV_OK;
+  // scale * log2(e), scale / cap and slope / scale stay normal numbers
+  return o->scale < 1e-10f || o->scale > 1e10f ? ECHOKV_ERR_SHAPE : ECHOKV_OK;
 }
 
 int check_table(const echokv_page_table* t) {
@@ -98,7 +99,7 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
               const echokv_score_extras* x, void* out, float* lse, const Schedule& s, page::AttnArgs* a) {
   if (!q || !out) return ECHOKV_ERR_NULL;
   if (!aligned16({q, out}) || ((uintptr_t)lse & 3)) return ECHOKV_ERR_SHAPE;
-  if (x && (!std::isfinite(x->softcap) || x->softcap < 0.f || x->softcap > 1e37f || (x->softcap > 0.f && x->softcap < 1e-30f))) return ECHOKV_ERR_SHAPE;
+  if (x && (!std::isfinite(x->softcap) || x->softcap < 0.f || x->softcap > 1e20f || (x->softcap > 0.f && x->softcap < 1e-20f))) return ECHOKV_ERR_SHAPE;
   *a = page::AttnArgs{};
   a->k = (const uint8_t*)c->k; a->v = (const uint8_t*)c->v; a->ke = c->k_exp; a->ve = c->v_exp;
   a->kt = (const bf16_t*)c->k_tail; a->vt = (const bf16_t*)c->v_tail; a->q = (const bf16_t*)q;

@@ -15,7 +15,6 @@
 namespace echokv {
 namespace page {
 
-typedef short frag_t __attribute__((ext_vector_type(8)));       // eight bf16
 typedef __bf16 bf16x8v_t __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ floatx4_t mfma(uint4 a, uint4 b, floatx4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v_t, a), __builtin_bit_cast(bf16x8v_t, b), c, 0, 0, 0);
@@ -35,7 +34,7 @@ struct AttnArgs {
   Plan plan;
   PlanKey key;
   float scale, cap, to_arg, tanh_k[4];  // to_arg: scale / cap; tanh_k: see score
-  int max_pages, n_pages, G, col_tiles, n_items;
+  int max_pages, n_pages, G, col_tiles;
 };
 
 // Maximum / sum over the four 16-lane rows, in every lane.

@@ -252,8 +252,12 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     for (int i = 0; i < S; ++i) s[i] = 0;
     s[FullHalves] = h[0];
   }
-  // halves per item: as many for each of its waves (decode, few columns); of a share of the keys
-  const auto chunk = [](double halves, int items, int waves) { const int64_t work = (int64_t)halves; return (int)max((int64_t)waves, (work + (int64_t)items * waves - 1) / ((int64_t)items * waves) * waves); };
+  // halves per item: as many for each of its waves (decode, few columns); of a share of the keys.  (At most 2^26, more than a sequence has: sequences may share pages,
+  // and the sum of their halves is bounded by nothing else.)
+  const auto chunk = [](double halves, int items, int waves) {
+    const int64_t work = (int64_t)halves, even = (work + (int64_t)items * waves - 1) / ((int64_t)items * waves) * waves;
+    return (int)min(max((int64_t)waves, even), (int64_t)1 << 26);
+  };
   const int dec_chunk = chunk(s[FullHalves], a.dec_items, 4);
   const int wide = (int)s[Wide], total = (int)s[Rows];
   const bool large = s[Large] * a.H_kv >= kPfMany || s[LargeHalves] * a.H_kv >= kPfFill * kPfLong;

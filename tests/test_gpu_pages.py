@@ -554,3 +554,38 @@ def test_a_prompt_in_chunks_then_tokens_and_back_to_a_layer_cache():
     side.synchronize()
     assert (other.cpu().float() - out.float()).abs().max() <= 2 * ref.HALF_BF16 * out.float().abs().max()
     assert (other_lse.cpu() - lse).abs().max() <= 1e-4
+
+
+def test_everything_is_refused_while_another_gpu_is_the_current_one(monkeypatch):
+    """Views of tables and caches that were made before, too; nothing is launched."""
+    b = Batch(GQA, 2).grow([130, 5])
+    q, (out, lse), space = b.random(2, b.hq, b.d).to(DEV), b.out(2), b.workspace()
+    which = torch.zeros(2, dtype=torch.int32, device=DEV)
+    ek.page_decode_attn(b.shape, b.table, b.cache, b.plan, q, out, lse, space)
+    torch.cuda.synchronize()
+    monkeypatch.setitem(ek._DTYPES, "device", lambda: 1)
+    for call in (lambda: ek.pages_release(b.table, which), lambda: ek.page_decode_attn(b.shape, b.table, b.cache, b.plan, q, out, lse, space),
+                 lambda: ek.page_append(b.shape, b.table, b.cache, b.plan, None, None), lambda: b.table.as_c(), lambda: b.plan.as_c(),
+                 lambda: b.cache.as_c(b.shape, b.table)):
+        with pytest.raises(ValueError, match="current GPU is cuda:1"):
+            call()
+    monkeypatch.undo()
+    with pytest.raises(ValueError, match="workspace"):
+        ek.page_decode_attn(b.shape, b.table, b.cache, b.plan, q, out, lse, space.cpu())
+    assert int(b.table.seq_len[0]) == 130
+
+
+def test_shares_of_more_halves_than_32_bits_hold():
+    """Sequences may share pages: 4096 of 2^19 halves each, one share for all of them.  The share's size stays within 2^26, more than any sequence has."""
+    batch, pages = 4096, 1 << 18
+    shape = ek.make_shape(1024, 1024, 64, 0, "bf16")
+    table = ek.PageTable(torch.empty(batch, pages, dtype=torch.int32, device=DEV), torch.full((batch,), pages * 128, dtype=torch.int32, device=DEV),
+                         torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV))
+    plan = ek.PagePlan.empty(batch, 8, DEV)
+    n_new = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    n_new[0] = n_new[7] = 4                                  # 4 columns each: two blocks of few
+    ek.pages_grow(shape, table, n_new, plan)
+    words = plan._words()[:16].tolist()
+    assert words[0] == 0 and words[2] == 1 << 26             # status, halves of a decode share
+    assert words[3] == batch + 2 and words[14] >= 2          # a share for each sequence's pages, tails of two of them; blocks of few columns
+    assert int(table.seq_len[0]) == pages * 128 + 4

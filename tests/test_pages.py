@@ -167,6 +167,30 @@ def test_views_follow_their_tensors():
     assert cache.as_c(SHAPE, t) is a and cache.as_c(ek.make_shape(8, 4, 128, 0, "bf16"), t) is not a
 
 
+def test_views_are_checked_again_when_another_gpu_is_the_current_one(monkeypatch):
+    class T:
+        shape = (9,)
+        def data_ptr(self): return FAKE
+    t = ek.PageTable(type("T2", (T,), dict(shape=(3, 7)))(), T(), T(), T())
+    monkeypatch.setitem(ek._DTYPES, "device", lambda: 0)
+    first = t.as_c()
+    assert t.as_c() is first
+    monkeypatch.setitem(ek._DTYPES, "device", lambda: 1)
+    assert t.as_c() is not first
+
+
+@pytest.mark.parametrize("scale", [1e-11, 1e-40, 1e11])
+def test_scales_of_scores_that_leave_the_range(scale):
+    shape = ek.make_shape(8, 2, 128, 0, "bf16", softmax_scale=scale)
+    assert codes(SHAPED, shape=shape) == {n: ek.ERR_SHAPE for n in SHAPED}
+    assert ek.page_workspace_bytes(shape, 2, 10) == 0
+
+
+@pytest.mark.parametrize("cap", [1e-21, 1e21, 1e37])
+def test_caps_that_leave_the_range(cap):
+    assert codes(ATTN, softcap=cap) == {n: ek.ERR_SHAPE for n in ATTN}
+
+
 def test_reference_rounding_and_scales():
     codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
     codes = torch.sort(codes[torch.isfinite(codes)]).values
