@@ -190,9 +190,13 @@ template <int STEP> struct PageWalk {
 
 // ---- decode: one token of every sequence.  A workgroup takes an item (a run of 64-token halves of a sequence's full pages, or its tail) of one KV
 // head and up to 16 of its query heads as columns.  Its four waves take the halves in turn, each with a softmax of its own; they are
-// joined in LDS.  What bounds it is the reading of the pages.
-constexpr int kDecodeItems = 1024;      // workgroups that the pages of a launch are shared out to
-constexpr int kNarrowItems = 256;      // the same of a prefill launch's few-column part
+// joined in LDS.  What bounds it is the reading of the pages: 8 x 4096 tokens of 32 KV heads 42 us, 131072 of 8 heads 43 us, both 6.3 TB/s (a plain streaming read: 6.2).
+// The matrix pipe has room to spare, so the probabilities go in as two bf16 numbers, high and low part: an error of 2^-17 of each for two products more.
+// Registers are the ring: 16 KB of codes in flight for a wave, eight waves to a compute unit.
+// kDecodeItems: workgroups that the pages of a launch are shared out to.  1024, 2048, 4096: 32 sequences of 256 .. 36864 tokens 97, 96, 96 us,
+// 2 x 131072 91, 96, 103; 512 is slower for the former.
+constexpr int kDecodeItems = 1024;
+constexpr int kNarrowItems = 256;       // the same of a prefill launch's few-column part: one round of its workgroups
 
 template <int HD, int MODE, typename TO>
 __global__ __launch_bounds__(256) void decode_kernel(AttnArgs a) {
@@ -393,7 +397,9 @@ __device__ __forceinline__ void join(const AttnArgs& a, const float* po, const f
   }
 }
 
-// One workgroup per (sequence, query head).  A sequence of one item is finished already; one of no tokens gets zeros and -inf.
+// One workgroup per (sequence, query head): 4 - 5 us behind the other launch.  A sequence of one item is finished already; one of no tokens gets zeros and -inf.
+// (Joined by the last workgroup of a row instead, no second launch: with fences at the GPU's scope 131072 tokens 49 -> 976 us, each of them writing back a whole L2; with
+// loads and stores past the L2 and no fence 8 x 4096 47 -> 77, the counter of a row being one word for workgroups on all dies.)
 template <int HD, typename TO>
 __global__ __launch_bounds__(256) void decode_merge_kernel(AttnArgs a) {
   if (!made_for(a.plan, a.key)) return;
@@ -411,6 +417,10 @@ __device__ __forceinline__ int parts_of(int tokens, int chunk) { return ((tokens
 // 48 to a wave, and walks the 64-token halves of the keys they see: codes to registers, widened to bf16 on their way into LDS
 // (once for all eight waves), operands back in the order of the lanes.  Two buffers, one barrier per half.  Where few blocks of queries face
 // long contexts the keys are split into shares, joined by a second launch.
+// The vector unit bounds it, beside the matrix pipe, with which it shares the SIMD's issue: per score an exponential of four slots, a multiply-add, a maximum, an addition,
+// half a conversion.  So the running maximum is a reference that is raised by 2^8 at a time, a bias starts the products' sums instead of following
+// them, masks cost nothing in halves that all columns see.  8192 causal queries, 32 heads of 128: 497 us = 1.11 PFLOP/s (a large library product: 1.21); 32
+// heads over 8: 544, with slopes 609, with a cap of 50 763, of 10 903.  48 columns to a wave are what its 256 registers hold.
 constexpr int kPfWaves = 8, kPfThreads = 64 * kPfWaves;
 constexpr float kRaise = 8.f;           // the reference of a softmax is raised once the maximum has passed it by 2^8: sums and outputs hold that
 
@@ -679,6 +689,8 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
 
 // Few columns: a workgroup takes up to 32 columns of one sequence and KV head and a run of halves, which its eight waves take in turn,
 // straight from memory to registers as in decode.  Waves that share halves instead of columns have work however few columns there are.
+// 49 rows behind 34396 tokens of 8 KV heads, four sequences: 34 us + the join's 5, where the bytes would take 12: a chain of four dependent loads to the first
+// half (plan, table, scale, codes), widening once per 32 columns, one round of workgroups.
 template <int HD, int MODE, typename TO>
 __device__ __forceinline__ void few_columns(const AttnArgs& a, int item, int kvh, uint4* lds) {
   constexpr int KS = HD / 32, KC = HD / 64, U = HD / 16, CT = kNCols / 16;

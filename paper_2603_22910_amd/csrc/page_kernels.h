@@ -16,7 +16,10 @@ constexpr int kTokens = 128;            // of a page
 constexpr int kMaxBatch = 4096;         // sequences: their prefix sums fit LDS
 constexpr int kMinExp = -100;           // least exponent of a scale: products of two of them and of a query stay normal numbers
 // (query, query head) columns of a prefill workgroup: 384, or 128 where those of 384 would be fewer than kPfMany with less than kPfLong halves for each compute
-// unit; 32 of a sequence of up to kNarrow.  (A half of 64 tokens costs 384 columns 3 us and 128 1.6.)
+// unit; 32 of a sequence of up to kNarrow.  A half of 64 tokens costs 384 columns 3 us and 128 1.6: large blocks have the rate, small ones fill the chip.  Measured
+// (32 query heads over 8 KV heads of 128, in us): kPfMany 320 against 512 or 900, 4001 queries: 162, 188; kPfLong 25, 40, 60: 512 queries behind 16384 tokens
+// 184, 184, 216, 16 x 60 behind 4000 124, 107, 105; kNarrow 64, 128, 256: 49 rows behind 34396 tokens in four sequences 51.6, 40.9, 39.8, 16 x 32 behind 4000
+// 83, 63.6, 63.2, 16 x 60 106, 109, 115.
 constexpr int kQCols = 384, kSCols = 128, kNCols = 32, kNarrow = 128, kPfMany = 320, kPfLong = 40;
 constexpr int kPfFill = 256;            // prefill workgroups that fill the chip, one to a compute unit: fewer are split over the keys
 
@@ -208,7 +211,9 @@ __device__ __forceinline__ Cut cut(int64_t n, int G, int many) {
 // A length's place among 256, eight to a factor of two.
 __device__ __forceinline__ int bucket(int t) { return (int)(__float_as_uint((float)t) >> 20) - (127 << 3); }
 
-// All or nothing: lengths, sums and chunk sizes by one workgroup, a thread per sequence.
+// All or nothing: lengths, sums and chunk sizes by one workgroup, a thread per sequence.  Every later choice needs sums over all sequences, so it is a chain of
+// loads, scans and barriers, 6 us for 32 sequences (8.6 a call) where an empty launch takes 3.9; 11 us for 512, and 5 for the 466 K slots and positions of their rows, which
+// a launch of their own writes then (up to 4096 rows by this workgroup: no second launch for a step).
 template <int NT>
 __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
   constexpr int S = 9;
@@ -487,7 +492,7 @@ __device__ __forceinline__ uint4 load_once(const uint4* p) {
 }
 
 // One workgroup per (item, KV head, side).  A block's rows are read once, into registers; its codes go through LDS into the page's order, 1 KB of
-// consecutive bytes per wave and store.  Item 0 of a sequence also moves the rows behind its last full block into the tail, after it has
+// consecutive bytes per wave and store.  Memory bounds it: 20542 rows of 4096 dims, both sides, 85 - 97 us = 5.2 - 5.9 TB/s of 3 bytes for a number.  Item 0 of a sequence also moves the rows behind its last full block into the tail, after it has
 // read the tail's old rows for the first block.
 template <int HD>
 __global__ __launch_bounds__(256, 4) void append_kernel(StoreArgs a) {
@@ -609,7 +614,8 @@ template <typename TO> __device__ __forceinline__ void put4bf(TO* p, uint32_t a,
 }
 
 // 128 rows of one KV head per workgroup.  Runs of at least kLongRun consecutive rows of a page are read in the page's order, 16 bytes a lane, and written
-// row by row; shorter ones, scattered rows and rows of tails are read where they are, all at once.
+// row by row; shorter ones, scattered rows and rows of tails are read where they are, all at once.  Memory bounds it: 20542 rows of 4096 dims 99 - 108 us = 4.7 - 5.1 TB/s.
+// (Storing and reading them took 295 us together with codes stored and rows read where each lies in the page's order.)
 constexpr int kLongRun = 16;
 template <int HD, typename TO>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs<TO> a) {
