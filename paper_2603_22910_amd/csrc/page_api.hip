@@ -64,7 +64,7 @@ int check_plan(const echokv_page_plan* p, const Sizes& z, int batch) {
 struct Schedule {
   int col_tiles, dec_items, pf_items, nw_items;
   int64_t dec_grid, pf_grid;                // items of a launch, at most
-  int64_t pf_parts, pf_small;               // of a split prefill launch with large or small blocks
+  int64_t pf_rows;                          // columns in a split prefill launch that leave partial results, of a KV head
   int64_t nw_grid, nw_parts;                // items of few columns, and those of them that leave partial results, at most
 };
 Schedule schedule(const Sizes& z, int batch, int max_rows) {
@@ -73,15 +73,18 @@ Schedule schedule(const Sizes& z, int batch, int max_rows) {
   s.dec_items = std::max(1, page::kDecodeItems / (z.H_kv * s.col_tiles));
   s.dec_grid = s.dec_items + 2 * (int64_t)batch;
   const int64_t cols = (int64_t)max_rows * z.G, seqs = std::min(batch, max_rows);
-  // blocks of 384 columns, or of 128 if there are fewer than kPfMany workgroups of the large ones (so at most three times as many small ones)
   const int64_t wide_seqs = cols > page::kNarrow ? std::min<int64_t>(seqs, cols / page::kNarrow) : 0, full = page::kPfFill / z.H_kv + 1;
-  const int64_t small = wide_seqs ? std::min<int64_t>(cols / page::kSCols + wide_seqs, 3 * (page::kPfMany / z.H_kv + 1)) : 0;
-  const int64_t large = wide_seqs ? cols / page::kQCols + wide_seqs : 0;
+  // blocks of 128 columns only where those of 384 (of 256 with a cap) are fewer than kPfMany, hence at most three times as many
+  const int64_t few = 3 * ((int64_t)page::kPfMany / z.H_kv + 1);
   // split: fewer blocks than fill the chip, and no more shares than that beside each block's last one
   s.pf_items = std::max(1, page::kPfFill / z.H_kv);
-  s.pf_parts = wide_seqs ? s.pf_items + std::min(large, full) : 0;
-  s.pf_small = wide_seqs ? s.pf_items + std::min(small, full) : 0;
-  s.pf_grid = std::max(std::max(large, small), std::max(s.pf_parts, s.pf_small));
+  s.pf_grid = s.pf_rows = 0;
+  for (int of : {page::kLCols, page::kMCols, page::kSCols}) {
+    if (!wide_seqs) break;
+    const int64_t all = cols / of + wide_seqs, n = of == page::kSCols ? std::min(all, few) : all, parts = s.pf_items + std::min(n, full);
+    s.pf_grid = std::max(s.pf_grid, std::max(n, parts));
+    s.pf_rows = std::max(s.pf_rows, parts * of);
+  }
   // A block whose keys are split has more halves than a share: there are at most as many such blocks as shares' worth of work
   s.nw_items = std::max(1, page::kNarrowItems / z.H_kv);
   s.nw_grid = s.nw_items + std::min(seqs * ((page::kNarrow + page::kNCols - 1) / page::kNCols), cols / page::kNCols + seqs);
@@ -114,6 +117,7 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
     if (arg > 1e-5 && arg < 1e4)
       for (int i = 0; i < 4; ++i) a->tanh_k[i] = (float)(k[i] * std::pow(arg, 2 * i + 1) * x->softcap * page::kLog2e);
   }
+  a->capped = x && x->softcap > 0.f;
   if (x) { a->cap = x->softcap; a->slopes = x->slopes; a->prefix = x->prefix_len; }
   return ECHOKV_OK;
 }
@@ -121,7 +125,7 @@ int attn_args(const Sizes& z, const echokv_page_table* t, const echokv_page_cach
 // Partials in the workspace: outputs, then (maximum, sum) pairs.
 size_t part_bytes(int64_t rows, int d) { return (size_t)rows * (d + 2) * 4; }
 
-int64_t wide_rows(const Sizes& z, const Schedule& s) { return std::max(s.pf_parts * page::kQCols, s.pf_small * page::kSCols) * z.H_kv; }
+int64_t wide_rows(const Sizes& z, const Schedule& s) { return s.pf_rows * z.H_kv; }
 int64_t prefill_rows(const Sizes& z, const Schedule& s) { return wide_rows(z, s) + s.nw_parts * page::kNCols * z.H_kv; }
 
 template <class F> int by_type(const Sizes& z, const page::AttnArgs& a, F f) {

@@ -34,7 +34,7 @@ struct AttnArgs {
   Plan plan;
   PlanKey key;
   float scale, cap, to_arg, tanh_k[4];  // to_arg: scale / cap; tanh_k: see score
-  int max_pages, n_pages, G, col_tiles;
+  int max_pages, n_pages, G, col_tiles, capped;
 };
 
 // Maximum / sum over the four 16-lane rows, in every lane.
@@ -414,13 +414,13 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(AttnArgs a) {
 __device__ __forceinline__ int parts_of(int tokens, int chunk) { return ((tokens + 63) / 64 - 1) / chunk + 1; }
 
 // ---- prefill: the queries of the new tokens.  A workgroup of eight waves takes 384 columns (query, query head of the KV head) of one sequence,
-// 48 to a wave, and walks the 64-token halves of the keys they see: codes to registers, widened to bf16 on their way into LDS
+// 48 to a wave (256, 32 or 128, 16: see grow_kernel), and walks the 64-token halves of the keys they see: codes to registers, widened to bf16 on their way into LDS
 // (once for all eight waves), operands back in the order of the lanes.  Two buffers, one barrier per half.  Where few blocks of queries face
 // long contexts the keys are split into shares, joined by a second launch.
 // The vector unit bounds it, beside the matrix pipe, with which it shares the SIMD's issue: per score an exponential of four slots, a multiply-add, a maximum, an addition,
 // half a conversion.  So the running maximum is a reference that is raised by 2^8 at a time, a bias starts the products' sums instead of following
 // them, masks cost nothing in halves that all columns see.  8192 causal queries, 32 heads of 128: 497 us = 1.11 PFLOP/s (a large library product: 1.21); 32
-// heads over 8: 544, with slopes 609, with a cap of 50 763, of 10 903.  48 columns to a wave are what its 256 registers hold.
+// heads over 8: 540, with slopes 604, with a cap of 50 686, of 10 809 (256 columns; of 384 765 and 903).  48 columns to a wave are what its 256 registers hold.
 constexpr int kPfWaves = 8, kPfThreads = 64 * kPfWaves;
 constexpr float kRaise = 8.f;           // the reference of a softmax is raised once the maximum has passed it by 2^8: sums and outputs hold that
 
@@ -457,11 +457,12 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
   const auto kbuf = [&](int hf) { return lds + (hf & 1) * (4 * KS * 64); };                   // halves as operands of 1 KB
   const auto vbuf = [&](int hf) { return lds + (2 * 4 * KS + (hf & 1) * (2 * U)) * 64; };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-  if (item >= a.plan.w[kPfItems]) return;
+  constexpr bool CAPPED = MODE == kCap || MODE == kCapBias;
+  if (item >= a.plan.blocks(CAPPED)[2]) return;
   const int H_q = a.key.H_q, G = a.G;
-  const int rank = find_item(a.plan.pf(), a.plan.w[kWideSeqs], item), item0 = a.plan.pf()[rank], b = __builtin_amdgcn_readfirstlane(a.plan.order()[rank]);
+  const int rank = find_item(a.plan.pf(CAPPED), a.plan.w[kWideSeqs], item), item0 = a.plan.pf(CAPPED)[rank], b = __builtin_amdgcn_readfirstlane(a.plan.order()[rank]);
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len = a.plan.len()[b], len0 = len - n;
-  const int chunk = a.plan.w[kPfChunk], shares = parts_of(len, chunk);
+  const int chunk = a.plan.blocks(CAPPED)[1], shares = parts_of(len, chunk);
   const int cols = n * G;                   // (below 2^31: the host sees to it)
   const int blocks = (cols - 1) / QC + 1, j = item - item0, share = j % shares;
   const int x0 = (blocks - 1 - j / shares) * QC;    // the longest ones first
@@ -561,9 +562,8 @@ __device__ __forceinline__ void many_columns(const AttnArgs& a, int item, int kv
   bool have = false;                      // probabilities of the half before
   // A step: products (values of the half before, keys of this one) and softmax.  Waves 0 .. 3 meet the barrier behind the softmax, waves 4 .. 7, which share
   // their SIMDs, behind the products: between two barriers the ones have the matrix pipe first and the others the vector unit.  The wave whose phase is the
-  // longer one goes first where both could issue (8192 queries, 32 heads: 515 us, without priorities 570, the other way round 564; with a cap 338, 358, 356).
+  // longer one goes first where both could issue (8192 queries, 32 heads: 515 us, without priorities 570, the other way round 564; with a cap, in blocks of 384, 338, 358, 356).
   const bool lag = wave >= 4;
-  constexpr bool CAPPED = MODE == kCap || MODE == kCapBias;
   const auto step = [&](int hf) {
     __builtin_amdgcn_s_setprio(CAPPED ? 0 : 1);
     const auto stage = [&](int part) {
@@ -902,7 +902,12 @@ __global__ __launch_bounds__(kPfThreads, 2) void prefill_kernel(AttnArgs a, int 
   __shared__ __attribute__((aligned(16))) uint4 lds[(2 * 4 * (HD / 32) + 2 * 2 * (HD / 16)) * 64];
   if (!made_for(a.plan, a.key)) return;
   const int kvh = blockIdx.x % a.key.H_kv, item = blockIdx.x / a.key.H_kv;
-  if (item < wide_items && a.plan.w[kCols] == kQCols) many_columns<HD, MODE, TO, 3>(a, item, kvh, lds);
+  constexpr bool CAPPED = MODE == kCap || MODE == kCapBias;
+  const int cols = a.plan.blocks(CAPPED)[0];
+  if constexpr (!CAPPED) {
+    if (item < wide_items && cols == kLCols) return many_columns<HD, MODE, TO, 3>(a, item, kvh, lds);
+  }
+  if (item < wide_items && cols == kMCols) many_columns<HD, MODE, TO, 2>(a, item, kvh, lds);
   else if (item < wide_items) many_columns<HD, MODE, TO, 1>(a, item, kvh, lds);
   else few_columns<HD, MODE, TO>(a, item - wide_items, kvh, lds);
 }
@@ -914,18 +919,18 @@ __global__ __launch_bounds__(256) void prefill_merge_kernel(AttnArgs a) {
   constexpr int L = HD / 4, GR = 64 / L;               // lanes of a row, rows at a time
   if (!made_for(a.plan, a.key)) return;
   const int B = a.key.batch, H_kv = a.key.H_kv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t units = (int64_t)a.plan.split()[B] * H_kv;
+  const int64_t units = (int64_t)a.plan.split(a.capped)[B] * H_kv;
   const bool whole = units <= kMergeBlocks;
   for (int64_t i = whole ? blockIdx.x : blockIdx.x * 4 + wave; i < units; i += whole ? gridDim.x : gridDim.x * 4) {
-    const int kvh = (int)(i % H_kv), at = (int)(i / H_kv), b = find_item(a.plan.split(), B, at), x = at - a.plan.split()[b];
-    const int row0 = a.plan.row_start()[b], cols = a.plan.split()[b + 1] - a.plan.split()[b], len = a.plan.len()[b];
+    const int kvh = (int)(i % H_kv), at = (int)(i / H_kv), b = find_item(a.plan.split(a.capped), B, at), x = at - a.plan.split(a.capped)[b];
+    const int row0 = a.plan.row_start()[b], cols = a.plan.split(a.capped)[b + 1] - a.plan.split(a.capped)[b], len = a.plan.len()[b];
     const bool narrow = cols <= kNarrow;
-    const int chunk = a.plan.w[narrow ? kNwChunk : kPfChunk], shares = parts_of(len, chunk), bc = narrow ? kNCols : a.plan.w[kCols];
+    const int chunk = narrow ? a.plan.w[kNwChunk] : a.plan.blocks(a.capped)[1], shares = parts_of(len, chunk), bc = narrow ? kNCols : a.plan.blocks(a.capped)[0];
     // what the column's block sees, hence its parts: a block of one is finished already
     const int last = min(x / bc * bc, cols - bc) + bc - 1, seen = max(len - cols / a.G + last / a.G + 1, a.prefix ? min(a.prefix[b], len) : 0);
     const int parts = parts_of(seen, chunk);
     if (parts == 1) continue;
-    const int first = narrow ? a.plan.nws()[b] + x / bc * shares : a.plan.pf_of()[b] + ((cols - 1) / bc - x / bc) * shares;
+    const int first = narrow ? a.plan.nws()[b] + x / bc * shares : a.plan.pf_of(a.capped)[b] + ((cols - 1) / bc - x / bc) * shares;
     const int64_t part = ((int64_t)first * H_kv + kvh) * bc + x % bc, stride = (int64_t)H_kv * bc;
     const float* po = (narrow ? a.nw_o : a.part_o) + part * HD;
     const float* pml = (narrow ? a.nw_ml : a.part_ml) + part * 2;

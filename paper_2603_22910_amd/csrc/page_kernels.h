@@ -15,17 +15,18 @@ namespace page {
 constexpr int kTokens = 128;            // of a page
 constexpr int kMaxBatch = 4096;         // sequences: their prefix sums fit LDS
 constexpr int kMinExp = -100;           // least exponent of a scale: products of two of them and of a query stay normal numbers
-// (query, query head) columns of a prefill workgroup: 384, or 128 where those of 384 would be fewer than kPfMany with less than kPfLong halves for each compute
-// unit; 32 of a sequence of up to kNarrow.  A half of 64 tokens costs 384 columns 3 us and 128 1.6: large blocks have the rate, small ones fill the chip.  Measured
-// (32 query heads over 8 KV heads of 128, in us): kPfMany 320 against 512 or 900, 4001 queries: 162, 188; kPfLong 25, 40, 60: 512 queries behind 16384 tokens
-// 184, 184, 216, 16 x 60 behind 4000 124, 107, 105; kNarrow 64, 128, 256: 49 rows behind 34396 tokens in four sequences 51.6, 40.9, 39.8, 16 x 32 behind 4000
-// 83, 63.6, 63.2, 16 x 60 106, 109, 115.
-constexpr int kQCols = 384, kSCols = 128, kNCols = 32, kNarrow = 128, kPfMany = 320, kPfLong = 40;
+// (query, query head) columns of a prefill workgroup: 384, 256 or 128; 32 of a sequence of up to kNarrow.
+constexpr int kLCols = 384, kMCols = 256, kSCols = 128, kNCols = 32, kNarrow = 128;
+// Large blocks at all: at least kPfMany of them over all KV heads, or kPfLong halves for each compute unit (kPfMany 512 or 900: 4001 queries 162 -> 188 us; kPfLong 25 and
+// 60: 16 x 60 behind 4000 107 -> 124, 512 behind 16384 184 -> 216).  Few columns: kNarrow 64 and 256: 49 rows behind 34396 tokens 41 -> 52, 16 x 60 109 -> 115.
+constexpr int kPfMany = 320, kPfLong = 40;
 constexpr int kPfFill = 256;            // prefill workgroups that fill the chip, one to a compute unit: fewer are split over the keys
 
 // ---- plan: what grow leaves for the other kernels, int32 words.  Words 16 on: row_start, then the arrays below, each of batch + 1 words.
-enum { kStatus, kWideSeqs, kDecChunk, kDecItems, kPfChunk, kPfItems, kAppItems, kFree0, kBatch, kHq, kHkv, kMaxRows, kMagic, kNwChunk, kNwItems, kCols, kHeadWords };
+// Prefill with a cap goes by a cut of its own (capped: 0 or 1), as its blocks are of other sizes: columns of a block, halves of a share, items.
+enum { kStatus, kWideSeqs, kDecChunk, kDecItems, kCols, kPfChunk, kPfItems, kFree0, kCapped, kMaxRows = 11, kMagic, kNwChunk, kNwItems, kHeads, kHeadWords };
 static_assert(kHeadWords == 16, "row_start's place is documented");
+struct Blocks { int cols, chunk, items; };
 constexpr int32_t kMagicWord = 0x45504732;
 struct Plan {
   int32_t* w;
@@ -36,19 +37,22 @@ struct Plan {
   __host__ __device__ int32_t* app() const { return arr(2); }            // prefix sums of append's items
   __host__ __device__ int32_t* dec() const { return arr(3); }            // ... of decode's items
   __host__ __device__ int32_t* fresh() const { return arr(4); }          // ... of the new pages
-  __host__ __device__ int32_t* pf() const { return arr(5); }             // ... of prefill's items of many columns, in the order of:
-  __host__ __device__ int32_t* order() const { return arr(6); }          // the sequences that have such, long ones first
-  __host__ __device__ int32_t* nw() const { return arr(7); }             // ... of its items of few columns
-  __host__ __device__ int32_t* nws() const { return arr(8); }            // ... of those that leave partial results
-  __host__ __device__ int32_t* split() const { return arr(9); }          // ... of the columns whose keys are split
-  __host__ __device__ int32_t* pf_of() const { return arr(10); }         // first of prefill's items of many columns, by sequence
-  static constexpr int kArrays = 11;
+  __host__ __device__ int32_t* nw() const { return arr(5); }             // ... of prefill's items of few columns
+  __host__ __device__ int32_t* nws() const { return arr(6); }            // ... of those that leave partial results
+  __host__ __device__ int32_t* order() const { return arr(7); }          // the sequences that have items of many columns, long ones first
+  __host__ __device__ int32_t* pf(int capped) const { return arr(8 + 3 * capped); }          // prefix sums of those items, in that order
+  __host__ __device__ int32_t* pf_of(int capped) const { return arr(9 + 3 * capped); }       // first of them, by sequence
+  __host__ __device__ int32_t* split(int capped) const { return arr(10 + 3 * capped); }      // prefix sums of the columns whose keys are split
+  static constexpr int kArrays = 14;
+  __device__ __forceinline__ int32_t* blocks(int capped) const { return w + kCols + (kCapped - kCols) * capped; }      // cols, chunk, items
 };
 
-// What the attention kernels make of a plan: sizes of the call that made it.
+// What the attention kernels make of a plan: sizes of the call that made it (batch below 2^13, H_q up to 2^16, H_kv up to 2^12).
 struct PlanKey { int batch, H_q, H_kv, max_rows; };
+__device__ __forceinline__ int32_t mark(int batch) { return kMagicWord ^ batch; }
+__device__ __forceinline__ int32_t heads_word(int H_q, int H_kv) { return H_q << 13 | H_kv; }
 __device__ __forceinline__ bool made_for(const Plan& p, const PlanKey& k) {
-  return p.w[kMagic] == kMagicWord && p.w[kBatch] == k.batch && p.w[kHq] == k.H_q && p.w[kHkv] == k.H_kv && p.w[kMaxRows] == k.max_rows;
+  return p.w[kMagic] == mark(k.batch) && p.w[kHeads] == heads_word(k.H_q, k.H_kv) && p.w[kMaxRows] == k.max_rows;
 }
 
 // The sequence that item x belongs to, by all lanes of a wave: how many of start[1 .. n] are at most x.
@@ -201,11 +205,10 @@ template <int N, int NT> __device__ __forceinline__ void block_scan(int32_t (&v)
 
 // Columns of a sequence with n new rows, and the blocks of `many` columns, or of few, that prefill cuts them into.
 struct Cut { bool narrow; int blocks; };
-__device__ __forceinline__ Cut cut(int64_t n, int G, int many) {
-  const int64_t cols = n * G;
-  const bool narrow = cols <= kNarrow;
-  const int c = narrow ? kNCols : many;
-  return {narrow, (int)((cols + c - 1) / c)};
+__device__ __forceinline__ Cut cut(int n, int G, int many) {       // n * G below 2^30
+  const uint32_t cols = n * G;
+  if (cols <= kNarrow) return {true, (int)((cols + kNCols - 1) / kNCols)};
+  return {false, (int)(many == kLCols ? (cols + kLCols - 1) / kLCols : many == kMCols ? (cols + kMCols - 1) / kMCols : (cols + kSCols - 1) / kSCols)};
 }
 
 // A length's place among 256, eight to a factor of two.
@@ -216,9 +219,9 @@ __device__ __forceinline__ int bucket(int t) { return (int)(__float_as_uint((flo
 // a launch of their own writes then (up to 4096 rows by this workgroup: no second launch for a step).
 template <int NT>
 __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
-  constexpr int S = 9;
-  __shared__ double red[S][NT / 64];
-  __shared__ int32_t wsum[7][NT / 64], hist[256];
+  constexpr int S = 5, X = 8;
+  __shared__ double red[X][NT / 64];
+  __shared__ int32_t wsum[8][NT / 64], hist[256], longest;
   __shared__ int32_t rows[NT + 1], lens[NT], fresh[NT];      // row_start, len, fresh, where the rows are looked at here
   const int tid = threadIdx.x, B = a.plan.n, G = a.H_q / a.H_kv;
   const int64_t cap = (int64_t)a.max_pages * kTokens + kTokens - 1;
@@ -227,24 +230,36 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
   if (tid < B) { first_l = a.len0[tid]; first_n = a.n_new[tid]; }
   const auto len_of = [&](int b) { return b == tid ? first_l : a.len0[b]; };
   const auto new_of = [&](int b) { return b == tid ? first_n : a.n_new[b]; };
-  enum { Rows, Pages, FullHalves, Small, SmallHalves, Large, LargeHalves, Wide, NarrowHalves };      // blocks of 128 and 384 columns, what they see at most
-  double s[S] = {0, 0, 0, 0, 0, 0, 0, 0, 0};
-  int wrong = 0;
+  // the sums s of all sequences and x of those of many columns: blocks of 128, 256 and 384 columns, the halves they see at most and without a prefix
+  enum { Rows, Pages, FullHalves, Wide, NarrowHalves }; enum { Small, Mid, Large, SmallHalves, MidHalves, LargeHalves, MidWork, LargeWork };
+  double s[S] = {0, 0, 0, 0, 0}, x[X] = {0, 0, 0, 0, 0, 0, 0, 0};
+  int wrong = 0, my_longest = 0;
+  if (tid == 0) longest = 0;
   for (int b = tid; b < B; b += NT) {
     const int64_t l = len_of(b), n = new_of(b);
     if (l < 0 || l > cap || n < 0) { wrong |= 1; continue; }      // ECHOKV_PLAN_BAD_LENGTH
     if (l + n > cap) { wrong |= 2; continue; }                    // ECHOKV_PLAN_TABLE_FULL
     const int64_t t = l + n, seen = (t + 63) / 64;
-    const Cut c = cut(n, G, kSCols);
+    const int rows = (int)min(n, (int64_t)a.max_rows);       // (more than that: nothing comes of it)
+    const Cut c = cut(rows, G, kSCols);
     s[Rows] += n; s[Pages] += t / kTokens - l / kTokens; s[FullHalves] += t / kTokens * 2;
     if (c.narrow) {
       s[NarrowHalves] += (double)c.blocks * seen;
     } else {
-      const int large = cut(n, G, kQCols).blocks;
-      s[Small] += c.blocks; s[SmallHalves] += (double)c.blocks * seen; s[Large] += large; s[LargeHalves] += (double)large * seen; s[Wide] += 1;
+      const int blocks[3] = {c.blocks, cut(rows, G, kMCols).blocks, cut(rows, G, kLCols).blocks};
+      for (int k = 0; k < 3; ++k) { x[Small + k] += blocks[k]; x[SmallHalves + k] += (double)blocks[k] * seen; }
+      const double mean = 0.5 * (double)(l / 64 + seen);
+      x[MidWork] += blocks[1] * mean; x[LargeWork] += blocks[2] * mean;
+      s[Wide] += 1;
+      my_longest = max(my_longest, (int)seen);
     }
   }
   block_sums<S, NT>(s, red);
+  if (s[Wide] > 0) {                                   // (a step of single tokens: none)
+    block_sums<X, NT>(x, red);
+    const int top = (int)wave_max64((float)my_longest);      // (below 2^24; 64 lanes' maxima one by one took 2.5 us)
+    if ((tid & 63) == 0) atomicMax(&longest, top);
+  }
   int status = (__syncthreads_or(wrong & 1) ? 1 : 0) | (__syncthreads_or(wrong & 2) ? 2 : 0);
   if (n_free0 < 0 || n_free0 > a.n_pages) status |= 1;
   if (!status && s[Pages] > n_free0) status |= 4;      // ECHOKV_PLAN_NO_PAGES
@@ -255,32 +270,50 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     for (int b = tid; b < B; b += NT) { const int64_t l = len_of(b); if (l >= 0 && l <= cap) h[0] += l / kTokens * 2; }
     block_sums<1, NT>(h, red);
     for (int i = 0; i < S; ++i) s[i] = 0;
+    for (int i = 0; i < X; ++i) x[i] = 0;
     s[FullHalves] = h[0];
   }
   // halves per item: as many for each of its waves (decode, few columns); of a share of the keys.  (At most 2^26, more than a sequence has: sequences may share pages,
   // and the sum of their halves is bounded by nothing else.)
+  // (The quotient is exact: whole numbers below 2^49 and 2^13.  A division of 64-bit integers would be some hundred instructions, fetched for this one use.)
   const auto chunk = [](double halves, int items, int waves) {
-    const int64_t work = (int64_t)halves, even = (work + (int64_t)items * waves - 1) / ((int64_t)items * waves) * waves;
-    return (int)min(max((int64_t)waves, even), (int64_t)1 << 26);
+    return (int)fmin(fmax(ceil(halves / (double)(items * waves)), 1.0) * waves, 67108864.0);
   };
   const int dec_chunk = chunk(s[FullHalves], a.dec_items, 4);
   const int wide = (int)s[Wide], total = (int)s[Rows];
-  const bool large = s[Large] * a.H_kv >= kPfMany || s[LargeHalves] * a.H_kv >= kPfFill * kPfLong;
-  const int many = large ? kQCols : kSCols;
-  const bool split = wide && (large ? s[Large] : s[Small]) * a.H_kv < kPfFill;
+  // Large blocks have the rate, small ones fill the chip and end together.  A half of 64 tokens costs 384, 256 and 128 columns 3.1, 2.2 and 1.4 us with all compute
+  // units busy, the longest blocks among them, which start first and run on alone, 2.5, 1.8 and 1.4; with a cap of 50 4.4, 2.65 and 1.7, so that 384 are never worth it.
+  // In us, 32 query heads over 8 KV heads of 128, blocks of 384 | 256 | 128:
+  // 8192 queries 532 | 558 | 714, with the cap 766 | 684 | 889; 6 x 257 .. 4001 192 | 201 | 259, with the cap 267 | 244 | 302; 4001 160 | 149 | 184; 2000 89 | 69 | 57;
+  // 512 behind 16384 179 | 180 | 212; 12 heads over 2 of 64, 8192 435 | 381 | 505.
+  Blocks blk[2];
+  bool split[2];
+  for (int capped = 0; capped < 2; ++capped) {
+    int k = 0;                                         // 0, 1, 2: 128, 256, 384 columns
+    if (capped) {
+      if (x[Mid] * a.H_kv >= kPfMany || x[MidHalves] * a.H_kv >= kPfFill * kPfLong * 1.5) k = 1;
+    } else if (x[Large] * a.H_kv >= kPfMany || x[LargeHalves] * a.H_kv >= kPfFill * kPfLong) {
+      const double l = longest, mid = fmax(l * 1.8, x[MidWork] * a.H_kv * (2.2 / kPfFill)), large = fmax(l * 2.5, x[LargeWork] * a.H_kv * (3.1 / kPfFill));
+      k = x[Mid] * a.H_kv >= kPfFill && mid < large ? 1 : 2;
+    }
+    blk[capped] = {k == 0 ? kSCols : k == 1 ? kMCols : kLCols, 0x7fffffff, 0};
+    split[capped] = wide && x[Small + k] * a.H_kv < kPfFill;
+    if (split[capped]) blk[capped].chunk = chunk(x[SmallHalves + k], a.pf_items, 8);      // the even share, for now
+  }
+  const bool alike = blk[0].cols == blk[1].cols;
   // A block's last share is short, and one workgroup more than the chip holds at a time doubles a launch's time: of 1, 5/4, 6/4 and 7/4 times the even share, a
   // wave each, the first that leaves no more items than that, else twice the even share.
-  int nw_chunk = chunk(s[NarrowHalves], a.nw_items, 8), pf_chunk = 0x7fffffff;
-  for (int which = 0; which < 2; ++which) {
+  int nw_chunk = chunk(s[NarrowHalves], a.nw_items, 8);
+  for (int which = 0; which < (alike ? 2 : 3); ++which) {
     const bool narrow = which == 0;
-    const int unit = 8, slots = narrow ? a.nw_items : a.pf_items, even = narrow ? nw_chunk : chunk(large ? s[LargeHalves] : s[SmallHalves], a.pf_items, unit);
-    if (narrow ? even == unit : !split) continue;
+    const int capped = which == 2, unit = 8, slots = narrow ? a.nw_items : a.pf_items, even = narrow ? nw_chunk : blk[capped].chunk, many = blk[capped].cols;
+    if (narrow ? even == unit : !split[capped]) continue;
     const auto candidate = [&](int k) { return (even * (4 + k) / 4 + unit - 1) / unit * unit; };
     const int wave = tid >> 6;
     if (wave < 4) {
       int64_t items = 0;
       for (int b = tid & 63; b < B; b += 64) {
-        const int64_t n = a.n_new[b];
+        const int n = a.n_new[b];
         const Cut c = cut(n, G, many);
         if (c.narrow == narrow && n) items += c.blocks * (((a.len0[b] + n + 63) / 64 - 1) / candidate(wave) + 1);
       }
@@ -290,15 +323,18 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     __syncthreads();
     int k = 0;
     while (k < 4 && red[0][k] > slots) ++k;
-    (narrow ? nw_chunk : pf_chunk) = candidate(k);
+    (narrow ? nw_chunk : blk[capped].chunk) = candidate(k);
     __syncthreads();
   }
-  const auto wide_items = [&](int b) {                 // from the plan: the lengths may have been overwritten in place
-    const int n = a.plan.row_start()[b + 1] - (b ? a.plan.row_start()[b] : 0), t = a.plan.len()[b];
-    const Cut c = cut(n, G, many);
-    return c.narrow ? 0 : c.blocks * (((t + 63) / 64 - 1) / pf_chunk + 1);
+  if (alike) blk[1] = blk[0];
+  const auto wide_items = [&](int b, const Blocks& x) {      // from what the plan got: the lengths may have been overwritten in place
+    const bool here = b < NT;
+    const int before = b == 0 ? 0 : here ? rows[b] : a.plan.row_start()[b], n = (here ? rows[b + 1] : a.plan.row_start()[b + 1]) - before;
+    const int t = here ? lens[b] : a.plan.len()[b];
+    const Cut c = cut(n, G, x.cols);
+    return c.narrow ? 0 : c.blocks * (((t + 63) / 64 - 1) / x.chunk + 1);
   };
-  int32_t carry[7] = {0, 0, 0, 0, 0, 0, 0};
+  int32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int b0 = 0; b0 < B; b0 += NT) {
     const int b = b0 + tid;
     int l = 0, n = 0;
@@ -309,30 +345,32 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
       a.len1[b] = ok ? l + n : (int)ll;
     }
     const int t = l + n, f0 = l / kTokens, f1 = t / kTokens, halves = f1 * 2, seen = (t + 63) / 64;
-    const Cut c = cut(n, G, many);
-    const int shares = n > 0 ? (seen - 1) / (c.narrow ? nw_chunk : pf_chunk) + 1 : 0, few = c.narrow ? c.blocks * shares : 0;
-    int32_t v[7];
+    const Cut c = cut(n, G, kSCols);
+    const auto shares = [&](int chunk) { return n > 0 ? (seen - 1) / (c.narrow ? nw_chunk : chunk) + 1 : 0; };
+    const int few = c.narrow ? c.blocks * shares(0) : 0;
+    int32_t v[8];
     v[0] = n;
     v[1] = n > 0 ? max(1, f1 - f0) : 0;
     v[2] = (halves + dec_chunk - 1) / dec_chunk + (t % kTokens ? 1 : 0);
     v[3] = f1 - f0;
     v[4] = few;
-    v[5] = shares > 1 ? few : 0;
-    v[6] = shares > 1 ? n * G : 0;
-    block_scan<7, NT>(v, carry, wsum);
+    v[5] = c.narrow && shares(0) > 1 ? few : 0;
+    v[6] = shares(blk[0].chunk) > 1 ? n * G : 0;
+    v[7] = shares(blk[1].chunk) > 1 ? n * G : 0;
+    block_scan<8, NT>(v, carry, wsum);
     if (b < B) {
       a.plan.row_start()[b + 1] = v[0]; a.plan.app()[b + 1] = v[1]; a.plan.dec()[b + 1] = v[2];
       a.plan.fresh()[b + 1] = v[3]; a.plan.nw()[b + 1] = v[4]; a.plan.nws()[b + 1] = v[5];
-      a.plan.split()[b + 1] = v[6];
+      a.plan.split(0)[b + 1] = v[6]; a.plan.split(1)[b + 1] = v[7];
       a.plan.len()[b] = t;
       if (b0 == 0) { rows[tid + 1] = v[0]; lens[tid] = t; fresh[tid] = v[3] - (f1 - f0); }
     }
   }
-  int32_t items[1] = {0};
+  int32_t items[2] = {0, 0};
   if (wide) {                                          // the longest sequences' blocks first: a long one that starts last would run on alone
     for (int i = tid; i < 256; i += NT) hist[i] = 0;
     __syncthreads();
-    for (int b = tid; b < B; b += NT) if (wide_items(b)) atomicAdd(&hist[bucket(a.plan.len()[b])], 1);
+    for (int b = tid; b < B; b += NT) if (wide_items(b, blk[0])) atomicAdd(&hist[bucket(a.plan.len()[b])], 1);
     __syncthreads();
     if (tid < 64) {                                    // places of the buckets, from the last one down
       int x[4], sum = 0;
@@ -343,23 +381,24 @@ __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
     }
     __syncthreads();
     // (which of two of a bucket comes first is a matter of chance, and of none to any result)
-    for (int b = tid; b < B; b += NT) if (wide_items(b)) a.plan.order()[atomicAdd(&hist[bucket(a.plan.len()[b])], 1)] = b;
+    for (int b = tid; b < B; b += NT) if (wide_items(b, blk[0])) a.plan.order()[atomicAdd(&hist[bucket(a.plan.len()[b])], 1)] = b;
     __syncthreads();
     for (int r0 = 0; r0 < wide; r0 += NT) {
       const int r = r0 + tid;
-      int32_t w[1] = {0};
-      int b = 0, mine = 0;
-      if (r < wide) { b = a.plan.order()[r]; w[0] = mine = wide_items(b); }
-      block_scan<1, NT>(w, items, wsum);
-      if (r < wide) { a.plan.pf()[r + 1] = w[0]; a.plan.pf_of()[b] = w[0] - mine; }
+      int32_t w[2] = {0, 0}, mine[2];
+      const int b = r < wide ? a.plan.order()[r] : 0;
+      for (int k = 0; k < 2; ++k) mine[k] = w[k] = r < wide ? wide_items(b, blk[k]) : 0;
+      block_scan<2, NT>(w, items, wsum);
+      for (int k = 0; k < 2; ++k) if (r < wide) { a.plan.pf(k)[r + 1] = w[k]; a.plan.pf_of(k)[b] = w[k] - mine[k]; }
     }
   }
   if (tid == 0) {
     int32_t* w = a.plan.w;
-    for (int i : {0, 2, 3, 4, 5, 7, 8, 9}) a.plan.arr(i)[0] = 0;
-    w[kStatus] = status; w[kWideSeqs] = wide; w[kDecChunk] = dec_chunk; w[kDecItems] = carry[2]; w[kPfChunk] = pf_chunk; w[kPfItems] = items[0];
-    w[kAppItems] = carry[1]; w[kFree0] = n_free0; w[kNwChunk] = nw_chunk; w[kNwItems] = carry[4]; w[kCols] = large ? kQCols : kSCols;
-    w[kBatch] = B; w[kHq] = a.H_q; w[kHkv] = a.H_kv; w[kMaxRows] = a.max_rows; w[kMagic] = kMagicWord;
+    for (int i : {0, 2, 3, 4, 5, 6, 8, 10, 11, 13}) a.plan.arr(i)[0] = 0;
+    w[kStatus] = status; w[kWideSeqs] = wide; w[kDecChunk] = dec_chunk; w[kDecItems] = carry[2];
+    w[kFree0] = n_free0; w[kNwChunk] = nw_chunk; w[kNwItems] = carry[4];
+    for (int k = 0; k < 2; ++k) { int32_t* x = a.plan.blocks(k); x[0] = blk[k].cols; x[1] = blk[k].chunk; x[2] = items[k]; }
+    w[kMaxRows] = a.max_rows; w[kHeads] = heads_word(a.H_q, a.H_kv); w[kMagic] = mark(B);
     *a.n_free1 = n_free0 - (int)s[Pages];
     rows[0] = 0;
   }
@@ -502,7 +541,7 @@ __global__ __launch_bounds__(256, 4) void append_kernel(StoreArgs a) {
   __shared__ float wmax[4];
   const int tid = threadIdx.x, wave = tid >> 6;
   const int side = blockIdx.x & 1, kvh = (blockIdx.x >> 1) % a.key.H_kv, item = (blockIdx.x >> 1) / a.key.H_kv;
-  if (!made_for(a.plan, a.key) || item >= a.plan.w[kAppItems]) return;
+  if (!made_for(a.plan, a.key) || item >= a.plan.app()[a.key.batch]) return;
   const int b = find_item(a.plan.app(), a.key.batch, item), j = item - a.plan.app()[b];
   const int row0 = a.plan.row_start()[b], n = a.plan.row_start()[b + 1] - row0, len1 = a.plan.len()[b], len0 = len1 - n;
   const int f0 = len0 / kTokens, f1 = len1 / kTokens;

@@ -589,3 +589,29 @@ def test_shares_of_more_halves_than_32_bits_hold():
     assert words[0] == 0 and words[2] == 1 << 26             # status, halves of a decode share
     assert words[3] == batch + 2 and words[14] >= 2          # a share for each sequence's pages, tails of two of them; blocks of few columns
     assert int(table.seq_len[0]) == pages * 128 + 4
+
+
+@pytest.mark.parametrize("layer,ctx,new,plain,capped", [
+    ((32, 32, 64), 0, 3600, 256, 256),                      # 320 blocks of 384, 480 of 256, whose longest ends earlier
+    ((32, 8, 64), 16384, 600, 384, 256),                    # few blocks, their keys split
+    ((32, 8, 64), 7, 600, 128, 128),
+    ((16, 16, 128), 100, 1290, 128, 128),
+    ((8, 8, 128), 0, 16400, 256, 256),                      # 344 and 520 blocks: the longest of 384 would take 257 x 2.5 us, all of 256 take 574
+    ((32, 32, 64), 0, 8192, 384, 256)])                     # 704 and 1024 blocks
+def test_blocks_of_every_size_with_and_without_a_cap(layer, ctx, new, plain, capped):
+    """Two dozen of a prompt's rows, the first and last ones and those at the blocks' edges among them."""
+    pages = (ctx + new) // 128 + 1
+    b = Batch(layer, 1, max_pages=pages, n_pages=pages, scale=0.25)
+    if ctx:
+        b.grow([ctx])
+    b.grow([new])
+    words = b.plan._words()[:16].tolist()
+    assert (words[4], words[8]) == (plain, capped)
+    q = b.random(new, b.hq, b.d)
+    some = sorted({0, 1, 31, 32, 63, 64, 95, 96, 127, 128, 255, 256, 383, 384, new // 2, new - 130, new - 129, new - 2, new - 1})
+    prefix = i32([ctx + 100])
+    for kw in (dict(), dict(softcap=8.0), dict(slopes=SLOPES(b.hq).to(DEV), softcap=8.0), dict(prefix_len=prefix), dict(prefix_len=prefix, softcap=8.0)):
+        out, lse = b.prefill(q, **kw)
+        slopes = kw.get("slopes")
+        b.check(out[some], lse[some], q[some], 0, [ctx + i for i in some], P_ONE, kw.get("softcap", 0.0), None if slopes is None else slopes.cpu(),
+                prefix=ctx + 100 if "prefix_len" in kw else 0)
