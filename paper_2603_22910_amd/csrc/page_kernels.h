@@ -215,8 +215,8 @@ __device__ __forceinline__ Cut cut(int n, int G, int many) {       // n * G belo
 __device__ __forceinline__ int bucket(int t) { return (int)(__float_as_uint((float)t) >> 20) - (127 << 3); }
 
 // All or nothing: lengths, sums and chunk sizes by one workgroup, a thread per sequence.  Every later choice needs sums over all sequences, so it is a chain of
-// loads, scans and barriers, 6 us for 32 sequences (8.6 a call) where an empty launch takes 3.9; 11 us for 512, and 5 for the 466 K slots and positions of their rows, which
-// a launch of their own writes then (up to 4096 rows by this workgroup: no second launch for a step).
+// loads, scans and barriers, 6 us for 32 sequences (8.6 a call) where an empty launch takes 3.9; 13 us for 512 prompts, and 5 for the 466 K slots and positions of
+// their rows, which a launch of their own writes then (up to 4096 rows by this workgroup: no second launch for a step).
 template <int NT>
 __global__ __launch_bounds__(NT) void grow_kernel(GrowArgs a) {
   constexpr int S = 5, X = 8;
