@@ -515,7 +515,8 @@ int echokv_pages_slots(const echokv_page_table *t, const int32_t *row_start,
 int echokv_pages_release(const echokv_page_table *t, const int32_t *which,
                          void *hip_stream);
 
-/* Store the new rows of one layer.  k_new, v_new : device [>= rows, D] bf16. */
+/* Store the new rows of one layer, once for each plan: rows of the tail that a block is
+ * completed from make room for the new tail.  k_new, v_new : device [>= rows, D] bf16. */
 int echokv_page_append(const echokv_shape *shape, const echokv_page_table *t,
                        const echokv_page_cache *c, const echokv_page_plan *plan,
                        const void *k_new, const void *v_new, void *hip_stream);

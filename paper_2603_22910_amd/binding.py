@@ -644,7 +644,7 @@ def pages_release(table: PageTable, which, stream=None):
 
 
 def page_append(shape: Shape, table: PageTable, cache: PageCache, plan: PagePlan, k_new, v_new, stream=None):
-    """k_new, v_new: bf16 [max_rows, n_kv_heads * d]; those behind the step's rows are not read."""
+    """Once for each plan and layer.  k_new, v_new: bf16 [max_rows, n_kv_heads * d]; those behind the step's rows are not read."""
     load()
     on = _gpu()
     least = plan.max_rows * shape.n_kv_heads * shape.head_dim

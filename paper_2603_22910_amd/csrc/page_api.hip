@@ -171,7 +171,7 @@ int echokv_pages_grow(const echokv_shape* shape, const echokv_page_table* t, con
   else if (t->batch <= 512) hipLaunchKernelGGL(page::grow_kernel<512>, dim3(1), dim3(512), 0, st, a);
   else hipLaunchKernelGGL(page::grow_kernel<1024>, dim3(1), dim3(1024), 0, st, a);
   LAUNCH_CHECK();
-  if (!a.rows_here) {
+  if (!a.rows_here && plan->max_rows > 0) {
     hipLaunchKernelGGL(page::grow_rows_kernel, dim3((plan->max_rows + page::kRowsPerBlock - 1) / page::kRowsPerBlock), dim3(page::kRowsPerBlock), 0, st, a);
     LAUNCH_CHECK();
   }

@@ -615,3 +615,21 @@ def test_blocks_of_every_size_with_and_without_a_cap(layer, ctx, new, plain, cap
         slopes = kw.get("slopes")
         b.check(out[some], lse[some], q[some], 0, [ctx + i for i in some], P_ONE, kw.get("softcap", 0.0), None if slopes is None else slopes.cpu(),
                 prefix=ctx + 100 if "prefix_len" in kw else 0)
+
+
+@pytest.mark.parametrize("batch", [1, 300, 1024, 1025, 4096])
+def test_plans_for_decode_alone(batch):
+    """max_rows = 0: nobody grows, lengths and decode's items stand; a token more than none is refused."""
+    b = Batch((4, 2, 64), batch, max_pages=2, n_pages=batch).grow([1 + i % 130 for i in range(batch)])
+    lens = b.table.seq_len.clone()
+    b.plan = ek.PagePlan.empty(batch, 0, DEV)
+    none = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    ek.pages_grow(b.shape, b.table, none, b.plan)
+    assert b.plan.status() == 0 and torch.equal(b.table.seq_len, lens) and not b.plan.row_start.any()
+    q = b.random(batch, b.hq, b.d)
+    out, lse = b.decode(q)
+    for i in (0, batch // 2, batch - 1):
+        b.check(out[i:i + 1], lse[i:i + 1], q[i:i + 1], i, [i % 130], P_PAIR)
+    none[batch - 1] = 1
+    ek.pages_grow(b.shape, b.table, none, b.plan)
+    assert b.plan.status() == ek.PLAN_TOO_MANY_ROWS and torch.equal(b.table.seq_len, lens)
